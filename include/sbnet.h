@@ -465,6 +465,76 @@ sbnet_status sbnet_conv_on_tiles_f8(const void *tiles_in_f8, const int32_t *coun
                                     float out_scale, void *tiles_out_bf16, void *stream);
 
 /*
+ * Root-mean-square norm over the channels of each pixel, with the residual's addition (a norm that needs no statistics
+ * of other pixels, so that a tile's result does not depend on which blocks are active; the units of Sec. 3.3 can take it in
+ * the place of batch normalisation).  A pixel's channels are one row; on the rows of the tiles b < min(*count, cap):
+ *   s = x + residual  (formed in fp32, rounded once to `dtype`; s = x without a residual),
+ *   y[c] = s[c] / sqrt(mean over c of s[c]^2 + eps) * gain[c]   (fp32 sums and arithmetic, one rounding).
+ * The norm is that of the rounded s, so that the two calls x + residual and norm give the same bits, and the gradient
+ * below needs s alone.  Later tiles of y and sum are not touched.
+ * x, residual, sum, y: [cap][pixels][C] in `dtype` (F32, BF16 or F16); residual and sum are both given or both NULL;
+ * gain: device float32 [C] or NULL (1); eps positive and finite.  C at most 32768; pointers need their element's
+ * alignment only, 16 bytes with C * element size a multiple of 16 is fastest.  sum may be x or residual, y may be x or
+ * residual, not both the same; other overlaps are refused.  A row whose squares pass float32's range gives zeros, one
+ * with an infinity or NaN gives NaN where it stands.
+ *
+ * sbnet_rms_norm_i8_on_tiles: the same s, and y in 8 bits, as sbnet_quantize_i8_on_tiles makes them of the unrounded
+ * (fp32) y.  codes: int8 [cap][pixels][pitch], scales: float32 [cap][pixels].
+ *
+ * sbnet_quantize_i8_on_tiles: one scale for each row v (a pixel's channels),
+ *   t = max(2^-100, max over c of |v[c]|),  scale = t / 127,  codes[c] = round(v[c] * (127 / t)) to nearest even, in fp32
+ * (both quotients rounded to fp32), so that v[c] is about codes[c] * scale; codes are in -127 .. 127.  pitch is C rounded up
+ * to a multiple of 16, and the codes behind C are written as 0.  A row that holds an infinity or NaN gets scale NaN and
+ * codes 0.
+ */
+sbnet_status sbnet_rms_norm_on_tiles(const void *x, const void *residual, sbnet_dtype dtype, const int32_t *count,
+                                     int cap, int pixels, int C, const float *gain, float eps, void *sum, void *y,
+                                     void *stream);
+sbnet_status sbnet_rms_norm_i8_on_tiles(const void *x, const void *residual, sbnet_dtype dtype, const int32_t *count,
+                                        int cap, int pixels, int C, const float *gain, float eps, void *sum,
+                                        int8_t *codes, float *scales, void *stream);
+sbnet_status sbnet_quantize_i8_on_tiles(const void *x, sbnet_dtype dtype, const int32_t *count, int cap, int pixels,
+                                        int C, int8_t *codes, float *scales, void *stream);
+
+/*
+ * Gradients of sbnet_rms_norm_on_tiles from s (its `sum`, or its x without a residual), dy = dL/dy and, where the sum is
+ * used past the norm, dsum = dL/ds of that use (NULL: none).  With r = 1 / sqrt(mean(s^2) + eps) and h = s * r, on the rows of
+ * the tiles b < min(*count, cap):
+ *   dx = r * (gain * dy - h * mean over c of (gain * dy * h)) + dsum    (the gradient of x and of the residual),
+ *   dgain[c] = sum over the rows of dy * h                              (device float32 [C], written; zeros without rows).
+ * fp32 sums and arithmetic, dx rounded once to `dtype`; dgain's sums in a fixed order, no atomics: the same bits every
+ * run for a given cap.  s, dy, dsum, dx: [cap][pixels][C]; later tiles of dx are not touched; dx may be s, dy or dsum (the
+ * whole stack; other overlaps are refused).  workspace: device, 4-byte aligned, sbnet_rms_norm_backward_workspace_bytes(cap, pixels, C)
+ * bytes, overwritten.
+ */
+size_t sbnet_rms_norm_backward_workspace_bytes(int cap, int pixels, int C);
+sbnet_status sbnet_rms_norm_backward_on_tiles(const void *s, const void *dy, const void *dsum, sbnet_dtype dtype,
+                                              const int32_t *count, int cap, int pixels, int C, const float *gain,
+                                              float eps, void *dx, float *dgain, void *workspace,
+                                              size_t workspace_bytes, void *stream);
+
+/*
+ * Pointwise (1x1, stride 1) convolution on tiles in 8-bit integers, with a scale for each pixel and each output channel:
+ *   out[b][p][o] = act(sum over c of codes[b][p][c] * w_codes[o][c] * (scales[b][p] * w_scales[o]) + bias[o]),
+ * act = ReLU when relu != 0, on the tiles b < min(*count, cap); later tiles are not touched.  The sum is exact (32-bit
+ * integers); it is then converted to fp32, multiplied by scales[b][p], then by w_scales[o], the bias added (each rounded
+ * to fp32), and the result rounded once to `dtype` (F32, BF16 or F16).  A NaN stays one through the ReLU.
+ * codes: int8 [cap][pixels][pitch] and scales: float32 [cap][pixels] as the two calls above write them; w_codes: int8
+ * [Cout][pitch], w_scales: float32 [Cout]; bias: float32 [Cout] or NULL; out: [cap][pixels][Cout].  pitch: the input channels
+ * rounded up to a multiple of 16 (the codes behind the last channel 0 on at least one side), at most 131056.  codes, w_codes and
+ * out 16-byte aligned.
+ *
+ * sbnet_quantize_weights_i8: w_hwio [1][1][Cin][Cout] in `dtype` -> w_codes [Cout][pitch], w_scales [Cout], each output
+ * channel's weights quantised as a row above.  Cin at most 131056.
+ */
+sbnet_status sbnet_quantize_weights_i8(const void *w_hwio, sbnet_dtype dtype, int Cin, int Cout, int8_t *w_codes,
+                                       float *w_scales, void *stream);
+sbnet_status sbnet_pointwise_i8_on_tiles(const int8_t *codes, const float *scales, const int32_t *count, int cap,
+                                         int pixels, int pitch, const int8_t *w_codes, const float *w_scales,
+                                         const float *bias, int Cout, int relu, sbnet_dtype dtype, void *out,
+                                         void *stream);
+
+/*
  * Backward pass of the residual branch of a bottleneck unit on tiles (Sec. 3.3; the forward branch is
  * sbnet_bottleneck_on_tiles), with the results, bit for bit, of the calls above: three weight, data and
  * bias gradients and two ReLU masks (where a convolution's kernel can, its stores are masked in place of a

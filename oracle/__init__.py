@@ -324,6 +324,49 @@ def conv_valid_f8(tile_codes, w_codes, bias=None, stride=1, relu=False, out_scal
 
 
 # ---------------------------------------------------------------------------------------
+# rows (a pixel's channels): root-mean-square norm, 8-bit codes with a scale per row, their product
+# ---------------------------------------------------------------------------------------
+def rms_norm(s, gain=None, eps=1e-6):
+    """s / sqrt(mean(s^2) + eps) * gain over the last axis."""
+    s = np.asarray(s, dtype=np.float64)
+    y = s / np.sqrt((s * s).mean(-1, keepdims=True) + float(np.float32(eps)))
+    return y if gain is None else y * np.asarray(gain, dtype=np.float64)
+
+
+def rms_norm_backward(s, dy, gain=None, dsum=None, eps=1e-6):
+    """(ds, dgain) of rms_norm for dL/dy, with dL/ds of other uses added to ds."""
+    s, dy = np.asarray(s, dtype=np.float64), np.asarray(dy, dtype=np.float64)
+    g = 1.0 if gain is None else np.asarray(gain, dtype=np.float64)
+    root = np.sqrt((s * s).mean(-1, keepdims=True) + float(np.float32(eps)))
+    ds = g * dy / root - s * (g * dy * s).mean(-1, keepdims=True) / root ** 3
+    if dsum is not None:
+        ds = ds + np.asarray(dsum, dtype=np.float64)
+    return ds, (dy * s / root).reshape(-1, s.shape[-1]).sum(0)
+
+
+def quantize_i8(v):
+    """(codes, scales) of the rows of v, in float32 as the quantiser is defined: t = max(2^-100, max |v|), scale = t / 127,
+    code = nearest even whole number to v * (127 / t); rows with an infinity or NaN: scale NaN, codes 0.  Rows of codes
+    are padded with zeros to a multiple of 16."""
+    v = np.asarray(v, dtype=np.float32)
+    fine = np.isfinite(v).all(-1)
+    v = np.where(fine[..., None], v, np.float32(0))
+    t = np.maximum(np.abs(v).max(-1), np.float32(2.0) ** -100)
+    codes = np.rint(v * (np.float32(127) / t)[..., None]).astype(np.int8)
+    pad = [(0, 0)] * (v.ndim - 1) + [(0, -v.shape[-1] % 16)]
+    return np.pad(codes, pad), np.where(fine, t / np.float32(127), np.float32(np.nan))
+
+
+def pointwise_i8(codes, scales, w_codes, w_scales, bias=None, relu=False):
+    """act(sum_c codes * w_codes * scale of the row * scale of the output channel + bias), in float64."""
+    acc = np.asarray(codes, dtype=np.float64) @ np.asarray(w_codes, dtype=np.float64).T
+    z = acc * np.asarray(scales, dtype=np.float64)[..., None] * np.asarray(w_scales, dtype=np.float64)
+    if bias is not None:
+        z = z + np.asarray(bias, dtype=np.float64)
+    return np.where(z < 0, 0.0, z) if relu else z
+
+
+# ---------------------------------------------------------------------------------------
 # compositions
 # ---------------------------------------------------------------------------------------
 def sparse_conv_tiled(x, idx, g_in, g_out, w, bias, y, stride=1, relu=False, add=False):

@@ -80,6 +80,14 @@ _SIGNATURES = {
     "sbnet_pack_weights_f8": (_ci, [_vp, _ci, _ci, _ci, _ci, _vp, ctypes.POINTER(_sz), _vp]),
     "sbnet_conv_on_tiles_f8": (_ci, [_vp, _vp, _ci, _ci, _ci, _ci, _vp, _vp, _ci, _ci, _ci, _ci, _ci, _ci,
                                      ctypes.c_float, _vp, _vp]),
+    "sbnet_rms_norm_on_tiles": (_ci, [_vp, _vp, _ci, _vp, _ci, _ci, _ci, _vp, ctypes.c_float, _vp, _vp, _vp]),
+    "sbnet_rms_norm_i8_on_tiles": (_ci, [_vp, _vp, _ci, _vp, _ci, _ci, _ci, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
+    "sbnet_quantize_i8_on_tiles": (_ci, [_vp, _ci, _vp, _ci, _ci, _ci, _vp, _vp, _vp]),
+    "sbnet_rms_norm_backward_workspace_bytes": (_sz, [_ci, _ci, _ci]),
+    "sbnet_rms_norm_backward_on_tiles": (_ci, [_vp, _vp, _vp, _ci, _vp, _ci, _ci, _ci, _vp, ctypes.c_float, _vp, _vp, _vp, _sz,
+                                               _vp]),
+    "sbnet_quantize_weights_i8": (_ci, [_vp, _ci, _ci, _ci, _vp, _vp, _vp]),
+    "sbnet_pointwise_i8_on_tiles": (_ci, [_vp, _vp, _vp, _ci, _ci, _ci, _vp, _vp, _vp, _ci, _ci, _ci, _vp, _vp]),
     "sbnet_bottleneck_forward_keep_on_tiles": (_ci, [_vp, _ci, _ci, _ci, _ci, _ci, _vp, _vp, _ci, _gp, _vp, _vp, _vp, _vp,
                                                      _vp, _vp, _vp, _vp, _vp, _vp]),
     "sbnet_bottleneck_backward_workspace_bytes": (_sz, [_ci, _ci, _ci, _ci, _ci, _ci]),
@@ -318,6 +326,40 @@ def pack_weights_f8(w_f8):
 def conv_on_tiles_f8(tiles_f8, count, w_packed, bias=None, stride=1, relu=False, out_scale=1.0, out=None):
     """Valid convolution of FP8 tiles [cap,th,tw,Cin] (uint8 codes) with FP8 weights -> bf16 [cap,th',tw',Cout]."""
     return _calls.conv_on_tiles_f8(tiles_f8, count, w_packed, bias, stride, relu, out_scale, out)
+
+
+def rms_norm_on_tiles(x, count, gain=None, residual=None, eps=1e-6, out=None, sum_out=None):
+    """(y, s): s = x + residual (x itself without one), y = s / sqrt(mean(s^2) + eps) * gain over the last dimension of the
+    active tiles of x [cap,...,C].  sum_out may be x or residual, out either of them too, but not the same one."""
+    return _calls.rms_norm_on_tiles(x, count, gain, residual, eps, out, sum_out)
+
+
+def rms_norm_i8_on_tiles(x, count, gain=None, residual=None, eps=1e-6, codes=None, scales=None, sum_out=None):
+    """(codes, scales, s): rms_norm_on_tiles with y in 8 bits, as quantize_i8_on_tiles makes them of the unrounded y."""
+    return _calls.rms_norm_i8_on_tiles(x, count, gain, residual, eps, codes, scales, sum_out)
+
+
+def rms_norm_backward_on_tiles(s, dy, count, gain=None, dsum=None, eps=1e-6, out=None, workspace=None):
+    """(dx, dgain) of rms_norm_on_tiles from its s and dL/dy; dsum = dL/ds of uses of the sum past the norm (added to dx).
+    dx is the gradient of x and of the residual, dgain float32 [C]."""
+    return _calls.rms_norm_backward_on_tiles(s, dy, count, gain, dsum, eps, out, workspace)
+
+
+def quantize_i8_on_tiles(x, count, codes=None, scales=None):
+    """x [cap,...,C] -> (int8 codes [cap,...,C rounded up to 16], float32 scales [cap,...]): x is about codes * scales, one scale
+    for each row of C values; rows beyond the active tiles are not written."""
+    return _calls.quantize_i8_on_tiles(x, count, codes, scales)
+
+
+def quantize_weights_i8(w_hwio):
+    """Weights [1,1,Cin,Cout] -> (int8 codes [Cout, Cin rounded up to 16], float32 scales [Cout]) for pointwise_i8_on_tiles."""
+    return _calls.quantize_weights_i8(w_hwio)
+
+
+def pointwise_i8_on_tiles(codes, scales, count, w_codes, w_scales, bias=None, relu=False, dtype=torch.bfloat16, out=None):
+    """1x1 convolution of 8-bit tiles (codes [cap,...,P], scales [cap,...]) with 8-bit weights (codes [Cout,P], scales [Cout]) ->
+    [cap,...,Cout] in `dtype` (or out's type): exact sums, then scaled, bias added, ReLU."""
+    return _calls.pointwise_i8_on_tiles(codes, scales, count, w_codes, w_scales, bias, relu, dtype, out)
 
 
 def bottleneck_forward_keep_on_tiles(tiles, indices, count, g_in, H, W, weights):

@@ -11,6 +11,7 @@
 #include <optional>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -433,6 +434,141 @@ PyObject *conv_f8(Args a) {                         // tiles_f8, count, w_packed
     return give(a[7], own);
 }
 
+// ---- calls on the rows of a stack [cap][...][C]: a row is the last dimension; the tensors of a call lie on one device, and it runs there
+struct Rows {
+    int cap, pixels, C;
+    at::DimVector lead;                             // every dimension but the last
+    Rows(const Tensor &t, const char *name) {
+        if (t.dim() < 2) raise(PyExc_ValueError, "%s must have two dimensions or more", name);
+        int64_t p = 1;
+        for (int64_t d = 0; d + 1 < t.dim(); ++d) {
+            lead.push_back(t.size(d));
+            if (d) p *= t.size(d);
+        }
+        const int64_t c = t.size(t.dim() - 1);
+        if (t.size(0) > INT32_MAX || p > INT32_MAX || c > INT32_MAX) raise(PyExc_ValueError, "%s is too large", name);
+        cap = (int)t.size(0); pixels = (int)p; C = (int)c;
+    }
+    at::DimVector with(int64_t last) const {
+        at::DimVector s = lead;
+        s.push_back(last);
+        return s;
+    }
+};
+
+const Tensor &shaped(const Tensor &t, at::IntArrayRef size, const char *what) {
+    require(t.sizes() == size, what);
+    return t;
+}
+const int32_t *count_of(PyObject *o) {
+    const Tensor &t = dev(o, "count", at::kInt);
+    require(t.numel() == 1, "count must hold one number");
+    return (const int32_t *)ptr(t);
+}
+void one_device(const Tensor &first, std::initializer_list<PyObject *> others) {
+    for (PyObject *o : others)
+        if (THPVariable_Check(o) && THPVariable_Unpack(o).device() != first.device()) raise(PyExc_ValueError, "the tensors must be on one device");
+}
+int64_t pitch_of(int64_t C) { return (C + 15) / 16 * 16; }
+
+// x, count, gain, residual, eps, out, sum_out; or, I8, x, count, gain, residual, eps, codes, scales, sum_out
+template <bool I8> PyObject *rms_norm(Args a) {
+    PyObject *so = a[I8 ? 7 : 6];
+    const Tensor &x = dev(a[0], "x");
+    const Rows r(x, "x");
+    one_device(x, {a[1], a[2], a[3], a[5], a[6], so});
+    const int32_t *cnt = count_of(a[1]);
+    const float *gain = vec(a[2], "gain", r.C);
+    const bool res = !none(a[3]);
+    if (res) shaped(dev(a[3], "residual", x.scalar_type()), x.sizes(), "shape of residual");
+    if (!res && !none(so)) raise(PyExc_ValueError, "sum_out needs a residual");
+    const float eps = f32(a[4]);
+    if (!none(so)) shaped(dev(so, "sum_out", x.scalar_type()), x.sizes(), "shape of sum_out");
+    Tensor o0, o1, os;
+    const Tensor &y = I8 ? shaped(output(a[5], "codes", r.with(pitch_of(r.C)), x, at::kChar, o0), r.with(pitch_of(r.C)), "shape of codes")
+                         : shaped(output(a[5], "out", x.sizes(), x, x.scalar_type(), o0), x.sizes(), "shape of out");
+    const Tensor *sc = I8 ? &shaped(output(a[6], "scales", r.lead, x, at::kFloat, o1), r.lead, "shape of scales") : nullptr;
+    const Tensor *s = res ? &output(so, "sum_out", x.sizes(), x, x.scalar_type(), os) : nullptr;
+    const void *rp = res ? ptr(THPVariable_Unpack(a[3])) : nullptr;
+    void *sp = s ? ptr(*s) : nullptr;
+    const c10::DeviceGuard guard(x.device());
+    if (I8)
+        call(sbnet_rms_norm_i8_on_tiles, (const void *)ptr(x), rp, dt_of(x), cnt, r.cap, r.pixels, r.C, gain, eps, sp, (int8_t *)ptr(y),
+             (float *)ptr(*sc), stream());
+    else
+        call(sbnet_rms_norm_on_tiles, (const void *)ptr(x), rp, dt_of(x), cnt, r.cap, r.pixels, r.C, gain, eps, sp, ptr(y), stream());
+    PyObject *sum = res ? give(so, os) : same(a[0]);
+    return I8 ? tuple(give(a[5], o0), give(a[6], o1), sum) : tuple(give(a[5], o0), sum);
+}
+
+PyObject *rms_norm_backward(Args a) {               // s, dy, count, gain, dsum, eps, out, workspace
+    const Tensor &s = dev(a[0], "s"), &dy = dev(a[1], "dy", s.scalar_type());
+    const Rows r(s, "s");
+    one_device(s, {a[1], a[2], a[3], a[4], a[6], a[7]});
+    shaped(dy, s.sizes(), "shape of dy");
+    const int32_t *cnt = count_of(a[2]);
+    const float *gain = vec(a[3], "gain", r.C);
+    const Tensor *ds = none(a[4]) ? nullptr : &shaped(dev(a[4], "dsum", s.scalar_type()), s.sizes(), "shape of dsum");
+    const float eps = f32(a[5]);
+    Tensor oo, own;
+    const Tensor &dx = shaped(output(a[6], "out", s.sizes(), s, s.scalar_type(), oo), s.sizes(), "shape of out");
+    size_t wb;
+    void *ws = space(a[7], s, sbnet_rms_norm_backward_workspace_bytes(r.cap, r.pixels, r.C), 4, own, &wb);
+    Tensor dgain = empty({r.C}, s, at::kFloat);
+    const c10::DeviceGuard guard(s.device());
+    call(sbnet_rms_norm_backward_on_tiles, (const void *)ptr(s), (const void *)ptr(dy), ds ? (const void *)ptr(*ds) : (const void *)nullptr, dt_of(s),
+         cnt, r.cap, r.pixels, r.C, gain, eps, ptr(dx), (float *)ptr(dgain), ws, wb, stream());
+    return tuple(give(a[6], oo), THPVariable_Wrap(dgain));
+}
+
+PyObject *quantize_i8(Args a) {                     // x, count, codes, scales
+    const Tensor &x = dev(a[0], "x");
+    const Rows r(x, "x");
+    one_device(x, {a[1], a[2], a[3]});
+    const int32_t *cnt = count_of(a[1]);
+    Tensor oc, os;
+    const at::DimVector size = r.with(pitch_of(r.C));
+    const Tensor &codes = shaped(output(a[2], "codes", size, x, at::kChar, oc), size, "shape of codes");
+    const Tensor &scales = shaped(output(a[3], "scales", r.lead, x, at::kFloat, os), r.lead, "shape of scales");
+    const c10::DeviceGuard guard(x.device());
+    call(sbnet_quantize_i8_on_tiles, (const void *)ptr(x), dt_of(x), cnt, r.cap, r.pixels, r.C, (int8_t *)ptr(codes), (float *)ptr(scales),
+         stream());
+    return tuple(give(a[2], oc), give(a[3], os));
+}
+
+PyObject *quantize_weights_i8(Args a) {             // w_hwio
+    const Tensor &w = dev(a[0], "w_hwio");
+    const Dims4 s(w, "w_hwio");
+    require(s.a == 1 && s.b == 1, "the weights must be those of a 1x1 convolution");
+    Tensor codes = empty({s.d, pitch_of(s.c)}, w, at::kChar), scales = empty({s.d}, w, at::kFloat);
+    const c10::DeviceGuard guard(w.device());
+    call(sbnet_quantize_weights_i8, (const void *)ptr(w), dt_of(w), s.c, s.d, (int8_t *)ptr(codes), (float *)ptr(scales), stream());
+    return tuple(THPVariable_Wrap(codes), THPVariable_Wrap(scales));
+}
+
+PyObject *pointwise_i8(Args a) {                    // codes, scales, count, w_codes, w_scales, bias, relu, dtype, out
+    const Tensor &t = dev(a[0], "codes", at::kChar), &w = dev(a[3], "w_codes", at::kChar);
+    const Rows r(t, "codes");
+    one_device(t, {a[1], a[2], a[3], a[4], a[5], a[8]});
+    const Tensor &sc = shaped(dev(a[1], "scales", at::kFloat), r.lead, "shape of scales");
+    const int32_t *cnt = count_of(a[2]);
+    require(w.dim() == 2 && w.size(1) == r.C && w.size(0) <= INT32_MAX, "shape of w_codes");
+    const int64_t n = w.size(0);
+    require(!none(a[4]), "w_scales");
+    const float *ws = vec(a[4], "w_scales", n), *bias = vec(a[5], "bias", n);
+    const int relu = flag(a[6]);
+    if (!THPDtype_Check(a[7])) raise(PyExc_TypeError, "dtype must be a torch.dtype");
+    const at::ScalarType dt = none(a[8]) ? reinterpret_cast<THPDtype *>(a[7])->scalar_type : dev(a[8], "out").scalar_type();
+    if (dt != at::kFloat && dt != at::kBFloat16 && dt != at::kHalf) raise(PyExc_TypeError, "unsupported dtype %s", c10::toString(dt));
+    Tensor own;
+    const at::DimVector size = r.with(n);
+    const Tensor &out = shaped(output(a[8], "out", size, t, dt, own), size, "shape of out");
+    const c10::DeviceGuard guard(t.device());
+    call(sbnet_pointwise_i8_on_tiles, (const int8_t *)ptr(t), (const float *)ptr(sc), cnt, r.cap, r.pixels, r.C, (const int8_t *)ptr(w), ws, bias,
+         (int)n, relu, dt_of(out), ptr(out), stream());
+    return give(a[8], own);
+}
+
 PyObject *conv_on_tiles(Args a) {                   // tiles, count, w_packed, bias, stride, relu, out
     const Tensor &t = dev(a[0], "tiles"), &cnt = dev(a[1], "count", at::kInt);
     const Packed w(a[2]);
@@ -725,6 +861,12 @@ PyMethodDef methods[] = {
     CALL("relu_bias_backward_on_tiles", relu_bias_backward, 5),
     CALL("quantize_f8", quantize_f8, 3),
     CALL("conv_on_tiles_f8", conv_f8, 8),
+    CALL("rms_norm_on_tiles", rms_norm<false>, 7),
+    CALL("rms_norm_i8_on_tiles", rms_norm<true>, 8),
+    CALL("rms_norm_backward_on_tiles", rms_norm_backward, 8),
+    CALL("quantize_i8_on_tiles", quantize_i8, 4),
+    CALL("quantize_weights_i8", quantize_weights_i8, 1),
+    CALL("pointwise_i8_on_tiles", pointwise_i8, 9),
     CALL("conv_on_tiles", conv_on_tiles, 7),
     CALL("conv_on_tiles_backward_data", backward_data, 8),
     CALL("conv_on_tiles_backward_weights", backward_weights, 7),
