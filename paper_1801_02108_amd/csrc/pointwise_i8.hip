@@ -22,7 +22,7 @@ __global__ __launch_bounds__(256) void i8_quantize_weights(const typename Elem<D
     for (int k = 0; k < 256; ++k) top = max(top, tops[k]);
     const RowCode rc = row_code(top);
     for (int c = threadIdx.x; c < pitch; c += 256)
-        codes[(size_t)o * pitch + c] = c < Cin ? (int8_t)code_of(Elem<DT>::load(w + (size_t)c * Cout + o), rc.inv) : (int8_t)0;
+        codes[(size_t)o * pitch + c] = c < Cin ? code1(Elem<DT>::load(w + (size_t)c * Cout + o), rc.inv, code_keep(top)) : (int8_t)0;
     if (threadIdx.x == 0) scales[o] = rc.scale;
 }
 

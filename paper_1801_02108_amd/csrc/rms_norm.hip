@@ -26,71 +26,91 @@ struct RowArgs {
     int cap, pixels, C, pitch;
 };
 
-__device__ __forceinline__ float add(float a, float b) { return a + b; }
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
+// T threads hold a row of up to T * P channels, E of them at a time; the workgroup has 256 threads or one row's.
+constexpr int wg_threads(int T) { return T < 256 ? 256 : T; }
 
-// over the 1024 threads of a workgroup, in a fixed order; `lds` holds 16 values and is free again after the next barrier
-template <typename V, typename F>
-__device__ __forceinline__ V over_workgroup(V v, F f, V *lds) {
-    for (int d = 32; d; d >>= 1) v = f(v, __shfl_xor(v, d));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
-    for (int w = 1; w < 16; ++w) v = f(v, lds[w]);
-    return v;
-}
-
-template <int DT, int FORM>
-__global__ __launch_bounds__(1024) void rms_rows(RowArgs p) {
-    typedef typename Elem<DT>::T T;
-    constexpr int P = kMaxC / 1024;
-    __shared__ float fl[16];
-    __shared__ uint32_t ul[16];
+template <int DT, int E, int T, int P, int FORM>
+__global__ __launch_bounds__(wg_threads(T)) void rms_rows(RowArgs p) {
+    constexpr int NV = P / E, RB = wg_threads(T) / T;
+    __shared__ uint32_t slots[2][2][16];
     const long long rows = active_rows(p.count, p.cap, p.pixels);
-    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
+    const int t = threadIdx.x % T;
+    float gain[P];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int c = (v * T + t) * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) gain[v * E + e] = 1.f;
+        if (FORM != kCodes && p.gain && c < p.C) load_floats<E>(gain + v * E, p.gain, c);
+    }
+    int turn = 0;
+    for (long long first = (long long)blockIdx.x * RB; first < rows; first += (long long)gridDim.x * RB, turn ^= 1) {
+        const long long row = first + threadIdx.x / T;
+        if (T <= 64 && row >= rows) break;                        // (a workgroup of one row has no such thread)
         const size_t at = (size_t)row * p.C;
-        float s[P], ss = 0.f;
+        Piece<DT, E> x[NV], res[NV];
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const int c = k * 1024 + threadIdx.x;
-            s[k] = 0.f;
-            if (c < p.C) {
-                s[k] = Elem<DT>::load((const T *)p.x + at + c);
-                if (FORM != kCodes && p.res) {
-                    T t;
-                    Elem<DT>::store(&t, s[k] + Elem<DT>::load((const T *)p.res + at + c));
-                    ((T *)p.sum)[at + c] = t;
-                    s[k] = Elem<DT>::load(&t);
-                }
-            }
-            ss += s[k] * s[k];
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * T + t) * E;
+            x[v].clear();
+            if (c < p.C) x[v].load(p.x, at + c);
         }
-        if (FORM != kCodes) {
-            const float r = rsqrtf(over_workgroup(ss, add, fl) * p.inv_c + p.eps);
+        if (FORM != kCodes && p.res) {
 #pragma unroll
-            for (int k = 0; k < P; ++k) {
-                const int c = k * 1024 + threadIdx.x;
-                if (c < p.C) s[k] = s[k] * r * (p.gain ? p.gain[c] : 1.f);
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * T + t) * E;
+                res[v].clear();
+                if (c < p.C) res[v].load(p.res, at + c);
             }
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * T + t) * E;
+                float sum[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e] = x[v].get(e) + res[v].get(e);
+                x[v].set(sum);
+                if (c < p.C) x[v].store(p.sum, at + c);
+            }
+        }
+        float s[P];
+#pragma unroll
+        for (int k = 0; k < P; ++k) s[k] = x[k / E].get(k % E);
+        if (FORM != kCodes) {
+            float ss = 0.f;
+#pragma unroll
+            for (int k = 0; k < P; ++k) ss += s[k] * s[k];
+            ss = __uint_as_float(over_row<T>(__float_as_uint(ss), AddF32(), slots[turn][0]));
+            const float r = rsqrtf(ss * p.inv_c + p.eps);
+#pragma unroll
+            for (int k = 0; k < P; ++k) s[k] = s[k] * r * gain[k];
         }
         if (FORM == kNorm) {
 #pragma unroll
-            for (int k = 0; k < P; ++k) {
-                const int c = k * 1024 + threadIdx.x;
-                if (c < p.C) Elem<DT>::store((T *)p.y + at + c, s[k]);
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * T + t) * E;
+                x[v].set(s + v * E);
+                if (c < p.C) x[v].store(p.y, at + c);
             }
         } else {
             uint32_t top = 0;
 #pragma unroll
             for (int k = 0; k < P; ++k) top = max(top, __float_as_uint(s[k]) & 0x7fffffffu);
-            const RowCode rc = row_code(over_workgroup(top, larger, ul));
+            top = over_row<T>(top, MaxU32(), slots[turn][1]);
+            const RowCode rc = row_code(top);
+            const uint32_t keep = code_keep(top);
+            int8_t *to = p.codes + (size_t)row * p.pitch;
 #pragma unroll
-            for (int k = 0; k < P; ++k) {
-                const int c = k * 1024 + threadIdx.x;
-                if (c < p.pitch) p.codes[(size_t)row * p.pitch + c] = (int8_t)code_of(s[k], rc.inv);
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * T + t) * E;
+                if (c >= p.pitch) continue;
+                if (E == 1) {
+                    to[c] = code1(s[v], rc.inv, keep);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; e += 4) *(uint32_t *)(to + c + e) = codes4(s + v * E + e, rc.inv, keep);
+                }
             }
-            if (threadIdx.x == 0) p.scales[row] = rc.scale;
+            if (t == 0) p.scales[row] = rc.scale;
         }
     }
 }
@@ -105,60 +125,146 @@ struct BackArgs {
     int cap, pixels, C;
 };
 
-template <int DT>
-__global__ __launch_bounds__(1024) void rms_backward_rows(BackArgs p) {
-    typedef typename Elem<DT>::T T;
-    constexpr int P = kMaxC / 1024;
-    __shared__ float fl[2][16];
+// A thread keeps its channels' sums of dy h over all its rows; the workgroup adds those of its rows' places in ascending order.
+template <int DT, int E, int T, int P>
+__global__ __launch_bounds__(wg_threads(T)) void rms_backward_rows(BackArgs p) {
+    constexpr int NV = P / E, RB = wg_threads(T) / T;
+    __shared__ uint32_t slots[2][2][16];
+    __shared__ float sums[RB > 1 ? RB * T * P : 1];
     const long long rows = active_rows(p.count, p.cap, p.pixels);
-    float dg[P];
+    const int t = threadIdx.x % T;
+    float gain[P], dg[P];
 #pragma unroll
-    for (int k = 0; k < P; ++k) dg[k] = 0.f;
-    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
-        const size_t at = (size_t)row * p.C;
-        float s[P], d[P], ss = 0.f, t = 0.f;
+    for (int v = 0; v < NV; ++v) {
+        const int c = (v * T + t) * E;
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const int c = k * 1024 + threadIdx.x;
-            s[k] = d[k] = 0.f;
-            if (c < p.C) {
-                s[k] = Elem<DT>::load((const T *)p.s + at + c);
-                d[k] = Elem<DT>::load((const T *)p.dy + at + c);
-                t += (p.gain ? p.gain[c] : 1.f) * d[k] * s[k];
-            }
-            ss += s[k] * s[k];
+        for (int e = 0; e < E; ++e) {
+            gain[v * E + e] = 1.f;
+            dg[v * E + e] = 0.f;
         }
-        const float r = rsqrtf(over_workgroup(ss, add, fl[0]) * p.inv_c + p.eps);
-        const float m = over_workgroup(t, add, fl[1]) * p.inv_c * r;
+        if (p.gain && c < p.C) load_floats<E>(gain + v * E, p.gain, c);
+    }
+    int turn = 0;
+    for (long long first = (long long)blockIdx.x * RB; first < rows; first += (long long)gridDim.x * RB, turn ^= 1) {
+        const long long row = first + threadIdx.x / T;
+        if (T <= 64 && row >= rows) break;                        // (a workgroup of one row has no such thread)
+        const size_t at = (size_t)row * p.C;
+        Piece<DT, E> s[NV], d[NV], past[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * T + t) * E;
+            s[v].clear();
+            d[v].clear();
+            past[v].clear();
+            if (c < p.C) {
+                s[v].load(p.s, at + c);
+                d[v].load(p.dy, at + c);
+                if (p.dsum) past[v].load(p.dsum, at + c);
+            }
+        }
+        float ss = 0.f, gs = 0.f;
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-            const int c = k * 1024 + threadIdx.x;
-            if (c < p.C) {
-                const float h = s[k] * r;
-                float dx = r * ((p.gain ? p.gain[c] : 1.f) * d[k] - h * m);
-                if (p.dsum) dx += Elem<DT>::load((const T *)p.dsum + at + c);
-                Elem<DT>::store((T *)p.dx + at + c, dx);
-                dg[k] += d[k] * h;
+            const float a = s[k / E].get(k % E);
+            ss += a * a;
+            gs += gain[k] * d[k / E].get(k % E) * a;
+        }
+        ss = __uint_as_float(over_row<T>(__float_as_uint(ss), AddF32(), slots[turn][0]));
+        gs = __uint_as_float(over_row<T>(__float_as_uint(gs), AddF32(), slots[turn][1]));
+        const float r = rsqrtf(ss * p.inv_c + p.eps), m = gs * p.inv_c * r;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * T + t) * E;
+            float dx[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float h = s[v].get(e) * r, dy = d[v].get(e);
+                dg[v * E + e] += dy * h;
+                dx[e] = r * (gain[v * E + e] * dy - h * m) + past[v].get(e);
             }
+            s[v].set(dx);
+            if (c < p.C) s[v].store(p.dx, at + c);
         }
     }
+    float *part = p.part + (size_t)blockIdx.x * p.C;
+    if (RB > 1) {
 #pragma unroll
-    for (int k = 0; k < P; ++k) {
-        const int c = k * 1024 + threadIdx.x;
-        if (c < p.C) p.part[(size_t)blockIdx.x * p.C + c] = dg[k];
+        for (int k = 0; k < P; ++k) sums[(threadIdx.x / T) * (T * P) + (k / E * T + t) * E + k % E] = dg[k];
+        __syncthreads();
+        for (int c = threadIdx.x; c < p.C; c += wg_threads(T)) {
+            float a = sums[c];
+#pragma unroll
+            for (int k = 1; k < RB; ++k) a += sums[k * (T * P) + c];
+            part[c] = a;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const int c = (k / E * T + t) * E + k % E;
+            if (c < p.C) part[c] = dg[k];
+        }
     }
 }
 
-__global__ __launch_bounds__(256) void rms_dgain_sum(const float *__restrict__ part, int n, int C, float *__restrict__ dgain) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= C) return;
-    float a = 0.f;
-    for (int k = 0; k < n; ++k) a += part[(size_t)k * C + c];
-    dgain[c] = a;
+// dgain[c] = sum over the workgroups' results part[w][c], w < n: 64 channels per workgroup of 16 waves; wave k takes the results
+// k, k + 16, ... in ascending order, eight loads in flight, then the 16 sums are added in ascending order
+__global__ __launch_bounds__(1024) void rms_dgain_sum(const float *__restrict__ part, int n, int C, float *__restrict__ dgain) {
+    __shared__ float slice[16][64];
+    const int lane = threadIdx.x & 63, k = threadIdx.x >> 6;
+    const int c = blockIdx.x * 64 + lane;
+    float acc = 0.f;
+    if (c < C) {
+        for (int b = k; b < n; b += 128) {
+            float a[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int bj = b + 16 * j;
+                const float v = part[(size_t)(bj < n ? bj : 0) * C + c];
+                a[j] = bj < n ? v : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc += a[j];
+        }
+    }
+    slice[k][lane] = acc;
+    __syncthreads();
+    if (k == 0 && c < C) {
+        float t = slice[0][lane];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) t += slice[i][lane];
+        dgain[c] = t;
+    }
+}
+
+// threads and channels per thread by the row's width, f(T, P) as types
+template <int A, int B> struct Split {
+    static constexpr int T = A, P = B;
+};
+template <typename F>
+void by_width(int C, F f) {
+    if (C <= 64) f(Split<8, 8>());
+    else if (C <= 128) f(Split<16, 8>());
+    else if (C <= 256) f(Split<32, 8>());
+    else if (C <= 512) f(Split<64, 8>());
+    else if (C <= 1024) f(Split<64, 16>());
+    else if (C <= 2048) f(Split<256, 8>());
+    else if (C <= 4096) f(Split<256, 16>());
+    else if (C <= 8192) f(Split<1024, 8>());
+    else if (C <= 16384) f(Split<1024, 16>());
+    else f(Split<1024, 32>());
 }
 
 // workgroups of the gradient: each leaves a row of partial sums
-int back_grid(long long rows) { return (int)(rows < 512 ? rows : 512); }
+int back_grid(long long rows, int C) {
+    int rb = 1, most = 512;
+    by_width(C, [&](auto w) {
+        constexpr int T = decltype(w)::T;
+        rb = wg_threads(T) / T;
+        most = T > 256 ? 512 : 1024;
+    });
+    const long long want = (rows + rb - 1) / rb;
+    return (int)(want < most ? want : most);
+}
 
 sbnet_status check_rows(const char *who, sbnet_dtype dtype, int cap, int pixels, int C, int most) {
     if (!is_float_dtype(dtype)) return fail(SBNET_EUNSUPPORTED, "%s: dtype must be f32, bf16 or f16", who);
@@ -172,6 +278,35 @@ sbnet_status check_rows(const char *who, sbnet_dtype dtype, int cap, int pixels,
 bool clash(const void *a, const void *b, size_t bytes) { return a && b && a != b && ranges_overlap(a, bytes, b, bytes); }
 
 bool eps_ok(float eps) { return eps > 0.f && eps * 0.f == 0.f; }
+
+template <int DT, int E>
+void rows_width(Form form, const RowArgs &p, size_t rows, hipStream_t s) {
+    by_width(form == kNorm ? p.C : p.pitch, [&](auto w) {         // (the codes fill the padding too)
+        constexpr int T = decltype(w)::T, P = decltype(w)::P, RB = wg_threads(T) / T;
+        const size_t want = (rows + RB - 1) / RB;
+        const int grid = (int)(want < 4096 ? want : 4096);
+        if (form == kNorm) hipLaunchKernelGGL((rms_rows<DT, E, T, P, kNorm>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
+        else if (form == kNormCodes) hipLaunchKernelGGL((rms_rows<DT, E, T, P, kNormCodes>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
+        else hipLaunchKernelGGL((rms_rows<DT, E, T, P, kCodes>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
+    });
+}
+template <int DT>
+void rows_form(Form form, bool wide, const RowArgs &p, size_t rows, hipStream_t s) {
+    if (wide) rows_width<DT, DT == SBNET_F32 ? 4 : 8>(form, p, rows, s);
+    else rows_width<DT, 1>(form, p, rows, s);
+}
+template <int DT, int E>
+void back_width(const BackArgs &p, int grid, hipStream_t s) {
+    by_width(p.C, [&](auto w) {
+        constexpr int T = decltype(w)::T, P = decltype(w)::P;
+        hipLaunchKernelGGL((rms_backward_rows<DT, E, T, P>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
+    });
+}
+template <int DT>
+void back_form(bool wide, const BackArgs &p, int grid, hipStream_t s) {
+    if (wide) back_width<DT, DT == SBNET_F32 ? 4 : 8>(p, grid, s);
+    else back_width<DT, 1>(p, grid, s);
+}
 
 sbnet_status rows_launch(const char *who, Form form, const void *x, const void *residual, sbnet_dtype dtype, const int32_t *count,
                          int cap, int pixels, int C, const float *gain, float eps, void *sum, void *y, int8_t *codes,
@@ -201,18 +336,12 @@ sbnet_status rows_launch(const char *who, Form form, const void *x, const void *
     RowArgs p = {};
     p.x = x; p.res = residual; p.sum = sum; p.y = y; p.codes = codes; p.scales = scales; p.gain = gain; p.count = count;
     p.eps = eps; p.inv_c = 1.f / (float)C; p.cap = cap; p.pixels = pixels; p.C = C; p.pitch = pitch;
-    const int grid = (int)(rows < 4096 ? rows : 4096);
-    hipStream_t s = (hipStream_t)stream;
-#define SBNET_ROWS(DT)                                                                                         \
-    do {                                                                                                       \
-        if (form == kNorm) hipLaunchKernelGGL((rms_rows<DT, kNorm>), dim3(grid), dim3(1024), 0, s, p);         \
-        else if (form == kNormCodes) hipLaunchKernelGGL((rms_rows<DT, kNormCodes>), dim3(grid), dim3(1024), 0, s, p); \
-        else hipLaunchKernelGGL((rms_rows<DT, kCodes>), dim3(grid), dim3(1024), 0, s, p);                      \
-    } while (0)
-    if (dtype == SBNET_F32) SBNET_ROWS(SBNET_F32);
-    else if (dtype == SBNET_BF16) SBNET_ROWS(SBNET_BF16);
-    else SBNET_ROWS(SBNET_F16);
-#undef SBNET_ROWS
+    const uintptr_t all = stacks | (uintptr_t)codes | (uintptr_t)gain;
+    const bool wide = (size_t)C * es % 16 == 0 && all % 16 == 0;
+    hipStream_t q = (hipStream_t)stream;
+    if (dtype == SBNET_F32) rows_form<SBNET_F32>(form, wide, p, rows, q);
+    else if (dtype == SBNET_BF16) rows_form<SBNET_BF16>(form, wide, p, rows, q);
+    else rows_form<SBNET_F16>(form, wide, p, rows, q);
     return launch_status(who);
 }
 
@@ -242,7 +371,7 @@ extern "C" sbnet_status sbnet_quantize_i8_on_tiles(const void *x, sbnet_dtype dt
 
 extern "C" size_t sbnet_rms_norm_backward_workspace_bytes(int cap, int pixels, int C) {
     if (cap < 0 || pixels <= 0 || C <= 0) return 0;
-    const int g = back_grid((long long)cap * pixels);
+    const int g = back_grid((long long)cap * pixels, C);
     return (size_t)(g > 0 ? g : 1) * C * sizeof(float);
 }
 
@@ -270,15 +399,16 @@ extern "C" sbnet_status sbnet_rms_norm_backward_on_tiles(const void *s, const vo
     BackArgs p = {};
     p.s = s; p.dy = dy; p.dsum = dsum; p.dx = dx; p.gain = gain; p.part = (float *)workspace; p.count = count;
     p.eps = eps; p.inv_c = 1.f / (float)C; p.cap = cap; p.pixels = pixels; p.C = C;
-    const int grid = back_grid((long long)cap * pixels);
+    const int grid = back_grid((long long)cap * pixels, C);
+    const bool wide = (size_t)C * es % 16 == 0 && (stacks | (uintptr_t)gain) % 16 == 0;
     hipStream_t q = (hipStream_t)stream;
     if (grid > 0) {
-        if (dtype == SBNET_F32) hipLaunchKernelGGL(rms_backward_rows<SBNET_F32>, dim3(grid), dim3(1024), 0, q, p);
-        else if (dtype == SBNET_BF16) hipLaunchKernelGGL(rms_backward_rows<SBNET_BF16>, dim3(grid), dim3(1024), 0, q, p);
-        else hipLaunchKernelGGL(rms_backward_rows<SBNET_F16>, dim3(grid), dim3(1024), 0, q, p);
+        if (dtype == SBNET_F32) back_form<SBNET_F32>(wide, p, grid, q);
+        else if (dtype == SBNET_BF16) back_form<SBNET_BF16>(wide, p, grid, q);
+        else back_form<SBNET_F16>(wide, p, grid, q);
         const sbnet_status done = launch_status(who);
         if (done != SBNET_OK) return done;
     }
-    hipLaunchKernelGGL(rms_dgain_sum, dim3((C + 255) / 256), dim3(256), 0, q, p.part, grid, C, dgain);
+    hipLaunchKernelGGL(rms_dgain_sum, dim3((C + 63) / 64), dim3(1024), 0, q, p.part, grid, C, dgain);
     return launch_status(who);
 }
