@@ -2,7 +2,7 @@
 // bias[o]), acc = sum over the channels of code * weight code, exact in 32 bits (131056 products of at most 2^14).
 //
 //   i8_quantize_weights  [1][1][Cin][Cout] -> [Cout][pitch] codes and a scale for each output channel
-//   i8_pointwise         the product
+//   i8_tiles, i8_direct  the product
 #include "rows.h"
 
 namespace sbnet {
@@ -32,32 +32,376 @@ struct PointArgs {
     const int32_t *count;
     void *out;
     int cap, pixels, pitch, N, relu;
+    int wide;                    // rows of out start at multiples of 16 bytes
 };
 
 __device__ __forceinline__ float finish(int acc, float a_scale, float w_scale, float bias, int relu) {
+#pragma clang fp contract(off)
     float v = (float)acc * a_scale;
-    v = __fadd_rn(__fmul_rn(v, w_scale), bias);
+    v = v * w_scale;
+    v = v + bias;
     return relu && v < 0.f ? 0.f : v;             // (a NaN stays one)
 }
 
-// 16 x 16 results per workgroup, one per thread, four products per instruction
+// ---- large products: tiles of BM rows x BN channels through LDS ----------------------------------------------------------
+// 32 x 32 x 32 steps of the matrix unit: its first operand is the weights (32 channels), its second the activations (32 rows), 16 bytes of
+// codes per lane each, so that a lane's 16 sums are channels of one row.  In LDS both operands are rows of 128 bytes, piece q of row i
+// at place q ^ (i / 2 % 8): the 16-byte reads of 16 neighbouring rows fall on different banks.  Row i of 32 weight rows is channel
+// 16 (i / 4 % 2) + 4 (i / 8) + i % 4, which makes a lane's sums 16 neighbouring channels.
+typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
+typedef __attribute__((__vector_size__(16 * sizeof(int)))) int i32x16;
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+typedef __attribute__((address_space(3))) void lds_void;
+
+__device__ __forceinline__ i32x16 mfma_i8(uint4 a, uint4 b, i32x16 c) {
+    return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint4 read16(const lds_byte *p) {
+    const u32x4 v = *(const __attribute__((address_space(3))) u32x4 *)p;
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ int channel_of_row(int i) { return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3); }
+
+// the results of 16 neighbouring channels of one row; `wide`: they all exist and 16-byte stores fit
 template <int DT>
-__global__ __launch_bounds__(256) void i8_pointwise(PointArgs p) {
-    const long long rows = active_rows(p.count, p.cap, p.pixels);
-    const long long row = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const int o = blockIdx.y * 16 + (threadIdx.x & 15);
-    if (row >= rows || o >= p.N) return;
-    const int4 *a = (const int4 *)(p.a + (size_t)row * p.pitch), *w = (const int4 *)(p.w + (size_t)o * p.pitch);
-    int acc = 0;
-    for (int k = 0; k < p.pitch / 16; ++k) {
-        const int4 u = a[k], v = w[k];
-        acc = __builtin_amdgcn_sdot4(u.x, v.x, acc, false);
-        acc = __builtin_amdgcn_sdot4(u.y, v.y, acc, false);
-        acc = __builtin_amdgcn_sdot4(u.z, v.z, acc, false);
-        acc = __builtin_amdgcn_sdot4(u.w, v.w, acc, false);
+__device__ __forceinline__ void store16(void *out, size_t at, const float *v, int left, bool wide) {
+    typedef typename Elem<DT>::T T;
+    if (wide) {
+        if (DT == SBNET_F32) {
+#pragma unroll
+            for (int k = 0; k < 16; k += 4) *(float4 *)((T *)out + at + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 16; k += 8)
+                *(uint4 *)((T *)out + at + k) = make_uint4(pack2<DT>(v[k], v[k + 1]), pack2<DT>(v[k + 2], v[k + 3]), pack2<DT>(v[k + 4], v[k + 5]),
+                                                           pack2<DT>(v[k + 6], v[k + 7]));
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            if (k < left) Elem<DT>::store((T *)out + at + k, v[k]);
     }
-    Elem<DT>::store((typename Elem<DT>::T *)p.out + (size_t)row * p.N + o,
-                    finish(acc, p.a_scales[row], p.w_scales[o], p.bias ? p.bias[o] : 0.f, p.relu));
+}
+
+constexpr int kStageK = 128;                      // bytes of a row in a stage
+
+// Waves 0 .. 3 multiply, WM x WN of them, each MF x NF blocks of 32 x 32; waves 4 .. 7 move the operands from memory to LDS, up to two stages ahead,
+// across the borders of tiles.  One barrier a stage: before it stage k has been read to the end and stage k + 1 has landed.
+template <int DT, int WM, int WN, int MF, int NF>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void i8_tiles(PointArgs p) {
+    constexpr int BM = WM * MF * 32, BN = WN * NF * 32;
+    constexpr int kStage = (BM + BN) * kStageK, kScales = (BM + 2 * BN) * 4;
+    constexpr int kCopies = (BM + BN) / 8 / 4;    // per moving wave and stage, 8 rows each
+    constexpr int kScaleCopies = (BM + 2 * BN) / 64, kScaleEach = (kScaleCopies + 3) / 4;
+    extern __shared__ __align__(16) char lds[];
+    lds_byte *const ldsb = (lds_byte *)lds;
+    lds_byte *const scaleb = ldsb + 3 * kStage;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long rows = active_rows(p.count, p.cap, p.pixels);
+    const int tm = (int)((rows + BM - 1) / BM), tn = (p.N + BN - 1) / BN, nk = (p.pitch + kStageK - 1) / kStageK;
+    // Tiles in bands of 8 along the rows, column by column; workgroups of one die (every eighth) take neighbouring ones, for its cache
+    const long long tiles = (long long)tm * tn;
+    const int G = gridDim.x;
+    const int place = G % 8 == 0 ? (int)(blockIdx.x % 8) * (G / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
+    const int mine = place < tiles ? (int)((tiles - place + G - 1) / G) : 0;
+    const int total = mine * nk;                  // stages
+    if (total == 0) return;
+    auto tile_at = [&](int j, long long &row0, int &n0) __attribute__((always_inline)) {
+        const long long pos = place + (long long)j * G, band = pos / (8LL * tn);
+        const int in = (int)(pos - band * 8 * tn), high = min(8, tm - (int)band * 8);
+        const int col = in / high;
+        row0 = (band * 8 + (in - col * high)) * BM;
+        n0 = col * BN;
+    };
+
+    if (wave >= 4) {
+        const int w = wave - 4;
+        uint32_t rel[kCopies];                    // copy w + 4 i of a stage: rows 8 (w + 4 i) ..
+        const uint32_t kb = (uint32_t)(((lane & 7) ^ ((w * 4 + (lane >> 4)) & 7)) * 16);
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int r = (w + 4 * i) * 8 + (lane >> 3);
+            const int src = r < BM ? r : ((r - BM) & ~31) + channel_of_row((r - BM) & 31);
+            rel[i] = (uint32_t)src * p.pitch + kb;
+        }
+        int j = -1, ks = nk;                      // the tile and stage in it that are requested next
+        long long row0 = 0;
+        int n0 = 0;
+        auto move = [&](int k) __attribute__((always_inline)) {
+            if (++ks >= nk) {
+                ks = 0;
+                ++j;
+                tile_at(j, row0, n0);
+            }
+            const uint32_t here = (uint32_t)min((long long)BM, rows - row0), wide = (uint32_t)min(BN, p.N - n0);
+            const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a + (size_t)row0 * p.pitch), 0, (int)(here * p.pitch), kBufWord3);
+            const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.w + (size_t)n0 * p.pitch), 0, (int)(wide * p.pitch), kBufWord3);
+            const uint32_t k0 = (uint32_t)ks * kStageK;
+            lds_byte *to = ldsb + (k % 3) * kStage + w * 1024;
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                // (bytes behind the row's end are the next row's: not fetched, and zero in LDS)
+                const uint32_t off = k0 + kb < (uint32_t)p.pitch ? rel[i] + k0 : kOutOfRange;
+                if (i * 32 < BM) __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)(to + i * 4096), 16, (int)off, 0, 0, 0);
+                else __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(to + i * 4096), 16, (int)off, 0, 0, 0);
+            }
+            if (ks == 0) {                        // the tile's scales and biases, 64 at a time
+                const __amdgpu_buffer_rsrc_t sr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a_scales + row0), 0, (int)(here * 4), kBufWord3);
+                const __amdgpu_buffer_rsrc_t cr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.w_scales + n0), 0, (int)(wide * 4), kBufWord3);
+                const __amdgpu_buffer_rsrc_t br = __builtin_amdgcn_make_buffer_rsrc((void *)(p.bias ? p.bias + n0 : p.w_scales), 0, p.bias ? (int)(wide * 4) : 0, kBufWord3);
+                lds_byte *st = scaleb + (j & 3) * kScales;
+#pragma unroll
+                for (int i = 0; i < kScaleEach; ++i) {
+                    const int c = min(w + 4 * i, kScaleCopies - 1);       // (every wave the same number: some do the last one again)
+                    if (c < BM / 64) __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, (lds_void *)(st + c * 256), 4, (c * 64 + lane) * 4, 0, 0, 0);
+                    else if (c < (BM + BN) / 64)
+                        __builtin_amdgcn_raw_ptr_buffer_load_lds(cr, (lds_void *)(st + c * 256), 4, ((c - BM / 64) * 64 + lane) * 4, 0, 0, 0);
+                    else __builtin_amdgcn_raw_ptr_buffer_load_lds(br, (lds_void *)(st + c * 256), 4, ((c - (BM + BN) / 64) * 64 + lane) * 4, 0, 0, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // until all but the newest stage has landed; a tile's first stage has its scales' copies too
+        auto wait = [&](bool newest, bool first) __attribute__((always_inline)) {
+            constexpr int A = kCopies, B = kCopies + kScaleEach;
+            if (!newest) __builtin_amdgcn_s_waitcnt(0x0F70);
+            else if (first) __builtin_amdgcn_s_waitcnt(0x0F70 | (B & 15) | ((B >> 4) << 14));
+            else __builtin_amdgcn_s_waitcnt(0x0F70 | (A & 15) | ((A >> 4) << 14));
+        };
+        move(0);
+        if (total > 1) move(1);
+        wait(total > 1, ks == 0);
+        __builtin_amdgcn_s_barrier();             // stage 0 is there
+        if (total > 2) move(2);
+        for (int k = 0; k < total; ++k) {
+            wait(k + 2 < total, ks == 0);         // stage k + 1
+            __builtin_amdgcn_s_barrier();
+            if (k + 3 < total) move(k + 3);
+        }
+    } else {
+        const int wm = wave / WN, wn = wave % WN;
+        const int l32 = lane & 31, h = lane >> 5;
+        uint32_t at[4];                           // this lane's piece of 32 rows at step 0 .. 3 of a stage
+#pragma unroll
+        for (int s = 0; s < 4; ++s) at[s] = (uint32_t)(l32 * 128 + (((2 * s + h) ^ ((l32 >> 1) & 7)) * 16));
+        const lds_byte *abase = ldsb + wm * MF * 4096, *wbase = ldsb + BM * 128 + wn * NF * 4096;
+        uint4 fa[2][MF], fw[2][NF];
+        auto fetch = [&](int set, const lds_byte *a, const lds_byte *w, int s) __attribute__((always_inline)) {
+#pragma unroll
+            for (int n = 0; n < NF; ++n) fw[set][n] = read16(w + at[s] + n * 4096);
+#pragma unroll
+            for (int m = 0; m < MF; ++m) fa[set][m] = read16(a + at[s] + m * 4096);
+        };
+        i32x16 acc[MF][NF];
+        auto multiply = [&](int set) __attribute__((always_inline)) {
+#pragma unroll
+            for (int m = 0; m < MF; ++m)
+#pragma unroll
+                for (int n = 0; n < NF; ++n) acc[m][n] = mfma_i8(fw[set][n], fa[set][m], acc[m][n]);
+        };
+        __syncthreads();                          // stage 0
+        fetch(0, abase, wbase, 0);
+        int k = 0, slot = 0;
+        for (int j = 0; j < mine; ++j) {
+#pragma unroll
+            for (int m = 0; m < MF; ++m)
+#pragma unroll
+                for (int n = 0; n < NF; ++n)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[m][n][e] = 0;
+            for (int ks = 0; ks < nk; ++ks, ++k) {
+                const lds_byte *a = abase + slot * kStage, *w = wbase + slot * kStage;
+                slot = slot == 2 ? 0 : slot + 1;
+                fetch(1, a, w, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(0);
+                __builtin_amdgcn_sched_barrier(0);
+                fetch(0, a, w, 2);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(1);
+                __builtin_amdgcn_sched_barrier(0);
+                fetch(1, a, w, 3);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(0);
+                __builtin_amdgcn_sched_barrier(0);
+                __syncthreads();                  // everything of this stage is in registers; the next one has landed
+                if (k + 1 < total) fetch(0, abase + slot * kStage, wbase + slot * kStage, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            long long row0;
+            int n0;
+            tile_at(j, row0, n0);
+            const float *sc = (const float *)(lds + 3 * kStage + (j & 3) * kScales);
+#pragma unroll
+            for (int m = 0; m < MF; ++m) {
+                const int r = (wm * MF + m) * 32 + l32;
+                const float as = sc[r];
+                const bool there = row0 + r < rows;
+                const size_t to = (size_t)(row0 + r) * p.N;
+#pragma unroll
+                for (int n = 0; n < NF; ++n) {
+                    const int c = (wn * NF + n) * 32 + 16 * h;
+                    float v[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[e] = finish(acc[m][n][e], as, sc[BM + c + e], sc[BM + BN + c + e], p.relu);
+                    if (there) store16<DT>(p.out, to + n0 + c, v, p.N - n0 - c, p.wide && n0 + c + 16 <= p.N);
+                }
+            }
+        }
+    }
+}
+
+// ---- small products: 16 MT rows x 16 NT channels per workgroup, operands from memory to registers, the channels summed over split between its waves
+// 16 x 16 x 64 steps, weights as the first operand again.  Wave w of KS takes the pieces of 128 bytes w, w + KS, ... of every row; the waves' sums
+// meet in LDS.  Frag n of NT holds channels 4 NT q + 4 n + r in its row 4 q + r, which gives a lane 4 NT neighbouring channels.
+// Bound by latency (few rows: by the weights' bytes): every wave has U pieces of all its rows in flight, twice.
+__device__ __forceinline__ i32x4 mfma_i8_16(uint4 a, uint4 b, i32x4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+}
+
+template <int DT>
+__device__ __forceinline__ void store4(void *out, size_t at, const float *v, int left, bool wide) {
+    typedef typename Elem<DT>::T T;
+    if (wide) {
+        if (DT == SBNET_F32) *(float4 *)((T *)out + at) = make_float4(v[0], v[1], v[2], v[3]);
+        else *(uint2 *)((T *)out + at) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < left) Elem<DT>::store((T *)out + at + k, v[k]);
+    }
+}
+
+template <int DT, int MT, int NT, int KS>
+__global__ __launch_bounds__(64 * KS) void i8_direct(PointArgs p) {
+    constexpr int U = MT + NT <= 2 ? 4 : MT + NT <= 4 ? 2 : 1;
+    constexpr int F = MT * NT;                    // fragments of 16 x 16
+    __shared__ int4 sums[KS][F][64];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long rows = active_rows(p.count, p.cap, p.pixels);
+    const int tm = (int)((rows + 16 * MT - 1) / (16 * MT));
+    // workgroups of one die (every eighth) take neighbouring tiles along the rows: they share weights
+    const int G = gridDim.x;
+    const int place = G % 8 == 0 ? (int)(blockIdx.x % 8) * (G / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
+    const int col = place / max(tm, 1), n0 = col * 16 * NT;
+    const long long row0 = (long long)(place - col * tm) * (16 * MT);
+    if (rows == 0 || n0 >= p.N) return;
+    const uint32_t here = (uint32_t)min(16LL * MT, rows - row0), wide = (uint32_t)min(16 * NT, p.N - n0);
+    const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a + (size_t)row0 * p.pitch), 0, (int)(here * p.pitch), kBufWord3);
+    const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.w + (size_t)n0 * p.pitch), 0, (int)(wide * p.pitch), kBufWord3);
+    // the results this thread finishes: fragment f of 64 lanes, 4 channels of a row
+    float as[(F + KS - 1) / KS], ws[(F + KS - 1) / KS][4], bs[(F + KS - 1) / KS][4];
+#pragma unroll
+    for (int i = 0; i < (F + KS - 1) / KS; ++i) {
+        const int f = wave + i * KS, m = f / NT, n = f % NT;
+        const int r = m * 16 + l16, c = 4 * NT * q + 4 * n;
+        as[i] = f < F && (uint32_t)r < here ? p.a_scales[row0 + r] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool ok = f < F && c + e < (int)wide;
+            ws[i][e] = ok ? p.w_scales[n0 + c + e] : 0.f;
+            bs[i][e] = ok && p.bias ? p.bias[n0 + c + e] : 0.f;
+        }
+    }
+    uint32_t arel[MT], wrel[NT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) arel[m] = (uint32_t)(m * 16 + l16) * p.pitch;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) wrel[n] = (uint32_t)(4 * NT * (l16 >> 2) + 4 * n + (l16 & 3)) * p.pitch;
+    const int pieces = (p.pitch + 127) / 128, mine = wave < pieces ? (pieces - wave + KS - 1) / KS : 0;
+    struct Ops { uint4 a[U][2][MT], w[U][2][NT]; };
+    auto load = [&](Ops &o, int i) __attribute__((always_inline)) {           // pieces i .. i + U - 1 of this wave; zeros behind the row's end
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint32_t k = (uint32_t)(wave + (i + u) * KS) * 128 + s * 64 + q * 16;
+                const bool in = k < (uint32_t)p.pitch;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) o.w[u][s][n] = buf_load16(wr, in ? wrel[n] + k : kOutOfRange);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) o.a[u][s][m] = buf_load16(ar, in ? arel[m] + k : kOutOfRange);
+            }
+    };
+    i32x4 acc[MT][NT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[m][n] = (i32x4){0, 0, 0, 0};
+    auto multiply = [&](const Ops &o) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[m][n] = mfma_i8_16(o.w[u][s][n], o.a[u][s][m], acc[m][n]);
+    };
+    Ops o0, o1;
+    if (mine > 0) load(o0, 0);
+    for (int i = 0; i < mine; i += 2 * U) {
+        if (i + U < mine) load(o1, i + U);
+        multiply(o0);
+        if (i + U < mine) {
+            if (i + 2 * U < mine) load(o0, i + 2 * U);
+            multiply(o1);
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sums[wave][m * NT + n][lane] = make_int4(acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < (F + KS - 1) / KS; ++i) {
+        const int f = wave + i * KS, m = f / NT, n = f % NT;
+        if (f >= F) break;
+        int4 t = sums[0][f][lane];
+#pragma unroll
+        for (int w = 1; w < KS; ++w) {
+            const int4 u = sums[w][f][lane];
+            t.x += u.x; t.y += u.y; t.z += u.z; t.w += u.w;
+        }
+        const int r = m * 16 + l16, c = n0 + 4 * NT * q + 4 * n;
+        const float v[4] = {finish(t.x, as[i], ws[i][0], bs[i][0], p.relu), finish(t.y, as[i], ws[i][1], bs[i][1], p.relu),
+                            finish(t.z, as[i], ws[i][2], bs[i][2], p.relu), finish(t.w, as[i], ws[i][3], bs[i][3], p.relu)};
+        if ((uint32_t)r < here) store4<DT>(p.out, (size_t)(row0 + r) * p.N + c, v, p.N - c, p.wide && c + 4 <= p.N);
+    }
+}
+
+template <int DT, int WM, int WN, int MF, int NF>
+sbnet_status tiles_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
+    constexpr int BM = WM * MF * 32, BN = WN * NF * 32, lds = 3 * (BM + BN) * kStageK + 4 * (BM + 2 * BN) * 4;
+    static_assert(lds <= 160 * 1024, "LDS");
+    const long long tiles = ((rows + BM - 1) / BM) * (((long long)p.N + BN - 1) / BN);
+    const int grid = (int)(tiles < 256 ? tiles : 256);
+    (void)hipFuncSetAttribute((const void *)i8_tiles<DT, WM, WN, MF, NF>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    hipLaunchKernelGGL((i8_tiles<DT, WM, WN, MF, NF>), dim3(grid), dim3(512), lds, s, p);
+    return launch_status(who);
+}
+
+template <int DT, int MT, int NT, int KS>
+sbnet_status direct_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
+    const long long tiles = (rows + 16 * MT - 1) / (16 * MT) * (((long long)p.N + 16 * NT - 1) / (16 * NT));
+    if (tiles >= 1LL << 30) return fail(SBNET_EUNSUPPORTED, "%s: too many output channels", who);
+    hipLaunchKernelGGL((i8_direct<DT, MT, NT, KS>), dim3((unsigned)tiles), dim3(64 * KS), 0, s, p);
+    return launch_status(who);
+}
+
+template <int DT>
+sbnet_status pointwise_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
+    if (rows * p.N >= 256LL * 256 * 128) return tiles_go<DT, 2, 2, 4, 2>(who, p, rows, s);
+    if (rows * p.N >= 64 * 128 * 128) return tiles_go<DT, 2, 2, 2, 2>(who, p, rows, s);
+    if (rows <= 16) return direct_go<DT, 1, 1, 8>(who, p, rows, s);
+    if (rows <= 32) return direct_go<DT, 2, 1, 8>(who, p, rows, s);
+    if (rows <= 64) return direct_go<DT, 2, 2, 4>(who, p, rows, s);
+    return direct_go<DT, 4, 2, 4>(who, p, rows, s);
 }
 
 }  // namespace
@@ -111,12 +455,9 @@ extern "C" sbnet_status sbnet_pointwise_i8_on_tiles(const int8_t *codes, const f
     PointArgs p = {};
     p.a = codes; p.w = w_codes; p.a_scales = scales; p.w_scales = w_scales; p.bias = bias; p.count = count; p.out = out;
     p.cap = cap; p.pixels = pixels; p.pitch = pitch; p.N = Cout; p.relu = relu ? 1 : 0;
-    const long long gy = ((long long)Cout + 15) / 16;
-    if (gy > 65535) return fail(SBNET_EUNSUPPORTED, "%s: too many output channels", who);
-    const dim3 grid((unsigned)((rows + 15) / 16), (unsigned)gy);
+    p.wide = (long long)Cout * elem_bytes(dtype) % 16 == 0;
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == SBNET_F32) hipLaunchKernelGGL(i8_pointwise<SBNET_F32>, grid, dim3(256), 0, s, p);
-    else if (dtype == SBNET_BF16) hipLaunchKernelGGL(i8_pointwise<SBNET_BF16>, grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL(i8_pointwise<SBNET_F16>, grid, dim3(256), 0, s, p);
-    return launch_status(who);
+    if (dtype == SBNET_F32) return pointwise_go<SBNET_F32>(who, p, (long long)rows, s);
+    if (dtype == SBNET_BF16) return pointwise_go<SBNET_BF16>(who, p, (long long)rows, s);
+    return pointwise_go<SBNET_F16>(who, p, (long long)rows, s);
 }
