@@ -375,6 +375,111 @@ __global__ __launch_bounds__(64 * KS) void i8_direct(PointArgs p) {
     }
 }
 
+// ---- long lists, few weights: a wave keeps the weights of 16 NT channels in registers and streams rows past them, 16 MT at a time
+// 16 x 16 x 64 steps.  A workgroup is `groups` waves of different channels times `streams` of different rows; waves of one stream read the same
+// rows at the same time.  Frags 2 s and 2 s + 1 hold channels 32 s + 8 q + 4 (n % 2) + r in their rows 4 q + r: a lane's pair is 8 neighbouring
+// channels, and one 16-byte store of a wave is 64 bytes of each of 16 rows.
+// Bound by memory: the next step's rows are requested before this one's are multiplied.
+template <int DT>
+__device__ __forceinline__ void store8(void *out, size_t at, const float *v, int left, bool wide) {
+    typedef typename Elem<DT>::T T;
+    if (wide) {
+        if (DT == SBNET_F32) {
+            *(float4 *)((T *)out + at) = make_float4(v[0], v[1], v[2], v[3]);
+            *(float4 *)((T *)out + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+            *(uint4 *)((T *)out + at) = make_uint4(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]), pack2<DT>(v[4], v[5]), pack2<DT>(v[6], v[7]));
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < left) Elem<DT>::store((T *)out + at + k, v[k]);
+    }
+}
+
+template <int DT, int KC, int NT, int MT>
+__global__ __launch_bounds__(256, 2) void i8_stream(PointArgs p, int groups, int streams) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long rows = active_rows(p.count, p.cap, p.pixels);
+    const int g = wave % groups;
+    const int n0 = ((int)blockIdx.y * groups + g) * 16 * NT;
+    long long row0 = ((long long)blockIdx.x * streams + wave / groups) * (16 * MT);
+    const long long stride = (long long)gridDim.x * streams * (16 * MT);
+    if (n0 >= p.N || row0 >= rows) return;
+    const uint32_t wide = (uint32_t)min(16 * NT, p.N - n0);
+    const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.w + (size_t)n0 * p.pitch), 0, (int)(wide * p.pitch), kBufWord3);
+    uint32_t arel[MT], k[KC];
+#pragma unroll
+    for (int i = 0; i < KC; ++i) k[i] = (uint32_t)(i * 64 + q * 16) < (uint32_t)p.pitch ? (uint32_t)(i * 64 + q * 16) : kOutOfRange;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) arel[m] = (uint32_t)(m * 16 + l16) * p.pitch;
+    struct Rows {
+        uint4 a[MT][KC];
+        float scale[MT];
+    };
+    auto load = [&](Rows &o, long long at) __attribute__((always_inline)) {
+        const uint32_t here = (uint32_t)min(16LL * MT, rows - at);
+        const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a + (size_t)at * p.pitch), 0, (int)(here * p.pitch), kBufWord3);
+        const __amdgpu_buffer_rsrc_t sr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a_scales + at), 0, (int)(here * 4), kBufWord3);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+            for (int i = 0; i < KC; ++i) o.a[m][i] = buf_load16(ar, arel[m] + k[i]);       // (out of range plus a row's offset stays out of range)
+            o.scale[m] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sr, (m * 16 + l16) * 4, 0, 0));
+        }
+    };
+    Rows o0, o1;
+    load(o0, row0);
+    uint4 w[NT][KC];
+    float ws[NT][4], bs[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t rel = (uint32_t)((n >> 1) * 32 + (l16 >> 2) * 8 + (n & 1) * 4 + (l16 & 3)) * p.pitch;
+#pragma unroll
+        for (int i = 0; i < KC; ++i) w[n][i] = buf_load16(wr, rel + k[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = n0 + (n >> 1) * 32 + q * 8 + (n & 1) * 4 + e;
+            ws[n][e] = c < p.N ? p.w_scales[c] : 0.f;
+            bs[n][e] = c < p.N && p.bias ? p.bias[c] : 0.f;
+        }
+    }
+    auto step = [&](const Rows &o, long long at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            i32x4 acc[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[n] = (i32x4){0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < KC; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[n] = mfma_i8_16(w[n][i], o.a[m][i], acc[n]);
+            const long long row = at + m * 16 + l16;
+#pragma unroll
+            for (int s = 0; s < NT / 2; ++s) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = finish(acc[2 * s + (e >> 2)][e & 3], o.scale[m], ws[2 * s + (e >> 2)][e & 3], bs[2 * s + (e >> 2)][e & 3], p.relu);
+                const int c = n0 + s * 32 + q * 8;
+                if (row < rows) store8<DT>(p.out, (size_t)row * p.N + c, v, p.N - c, p.wide && c + 8 <= p.N);
+            }
+        }
+    };
+    for (;;) {
+        const bool more = row0 + stride < rows;
+        if (more) load(o1, row0 + stride);
+        step(o0, row0);
+        if (!more) break;
+        row0 += stride;
+        const bool again = row0 + stride < rows;
+        if (again) load(o0, row0 + stride);
+        step(o1, row0);
+        if (!again) break;
+        row0 += stride;
+    }
+}
+
 template <int DT, int WM, int WN, int MF, int NF>
 sbnet_status tiles_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
     constexpr int BM = WM * MF * 32, BN = WN * NF * 32, lds = 3 * (BM + BN) * kStageK + 4 * (BM + 2 * BN) * 4;
@@ -394,8 +499,24 @@ sbnet_status direct_go(const char *who, const PointArgs &p, long long rows, hipS
     return launch_status(who);
 }
 
+template <int DT, int KC, int NT, int MT>
+sbnet_status stream_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
+    const int all = (p.N + 16 * NT - 1) / (16 * NT), gy = (all + 3) / 4, groups = (all + gy - 1) / gy, streams = 4 / groups;
+    const long long steps = (rows + 16 * MT * streams - 1) / (16 * MT * streams);
+    const int most = 512 / gy > 1 ? 512 / gy : 1;
+    hipLaunchKernelGGL((i8_stream<DT, KC, NT, MT>), dim3((unsigned)(steps < most ? steps : most), gy), dim3(64 * groups * streams), 0, s, p, groups, streams);
+    return launch_status(who);
+}
+
 template <int DT>
 sbnet_status pointwise_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
+    if (p.pitch <= 512 && p.N <= 512 && rows >= 8192) {
+        if (p.pitch <= 64) return stream_go<DT, 1, 4, 4>(who, p, rows, s);
+        if (p.pitch <= 128) return stream_go<DT, 2, 4, 4>(who, p, rows, s);
+        if (p.pitch <= 256) return stream_go<DT, 4, 4, 2>(who, p, rows, s);
+        if (p.pitch <= 384) return stream_go<DT, 6, 2, 2>(who, p, rows, s);
+        return stream_go<DT, 8, 2, 2>(who, p, rows, s);
+    }
     if (rows * p.N >= 256LL * 256 * 128) return tiles_go<DT, 2, 2, 4, 2>(who, p, rows, s);
     if (rows * p.N >= 64 * 128 * 128) return tiles_go<DT, 2, 2, 2, 2>(who, p, rows, s);
     if (rows <= 16) return direct_go<DT, 1, 1, 8>(who, p, rows, s);

@@ -315,6 +315,9 @@ PRODUCTS = [
     (65, 1, 2048, 256), (100, 1, 144, 48), (1, 127, 128, 128), (129, 1, 1024, 384), (3, 100, 64, 256), (4, 324, 256, 64), (5, 256, 384, 96),
     (2, 289, 80, 17), (11, 81, 112, 200), (1, 513, 4096, 130), (600, 1, 320, 1031), (1025, 1, 640, 264), (2, 1000, 32, 12), (1500, 1, 1168, 1100),
     (1, 1, 131056, 3), (130, 1, 131056, 40),
+    # long lists of narrow layers
+    (30, 324, 256, 64), (33, 256, 64, 250), (33, 256, 128, 130), (40, 256, 384, 96), (129, 64, 512, 40), (9001, 1, 16, 1), (36, 289, 80, 333),
+    (41, 256, 320, 512), (128, 81, 448, 200), (33, 255, 32, 513),
 ]
 
 
