@@ -375,10 +375,10 @@ __global__ __launch_bounds__(64 * KS) void i8_direct(PointArgs p) {
     }
 }
 
-// ---- long lists, few weights: a wave keeps the weights of 16 NT channels in registers and streams rows past them, 16 MT at a time
-// 16 x 16 x 64 steps.  A workgroup is `groups` waves of different channels times `streams` of different rows; waves of one stream read the same
-// rows at the same time.  Frags 2 s and 2 s + 1 hold channels 32 s + 8 q + 4 (n % 2) + r in their rows 4 q + r: a lane's pair is 8 neighbouring
-// channels, and one 16-byte store of a wave is 64 bytes of each of 16 rows.
+// ---- long lists, few weights: all weights lie in LDS, every wave streams rows past them, 16 MT at a time
+// 16 x 16 x 64 steps on 64 channels at a time.  The weights are laid out in LDS as the operand reads take them, 1 KB each, once a workgroup.  Frags 2 s
+// and 2 s + 1 hold channels 32 s + 8 q + 4 (n % 2) + r in their rows 4 q + r: a lane's pair is 8 neighbouring channels, and one 16-byte store of
+// a wave is 64 bytes of each of 16 rows.
 // Bound by memory: the next step's rows are requested before this one's are multiplied.
 template <int DT>
 __device__ __forceinline__ void store8(void *out, size_t at, const float *v, int left, bool wide) {
@@ -397,18 +397,18 @@ __device__ __forceinline__ void store8(void *out, size_t at, const float *v, int
     }
 }
 
-template <int DT, int KC, int NT, int MT>
-__global__ __launch_bounds__(256, 2) void i8_stream(PointArgs p, int groups, int streams) {
+constexpr int kStreamWaves = 8;
+
+template <int DT, int KC, int MT>
+__global__ __launch_bounds__(64 * kStreamWaves, 2) void i8_stream(PointArgs p, int groups) {
+    extern __shared__ __align__(16) char lds[];                   // [groups][KC][4] fragments of 1 KB, then scales and biases
+    lds_byte *const ldsb = (lds_byte *)lds;
     const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long rows = active_rows(p.count, p.cap, p.pixels);
-    const int g = wave % groups;
-    const int n0 = ((int)blockIdx.y * groups + g) * 16 * NT;
-    long long row0 = ((long long)blockIdx.x * streams + wave / groups) * (16 * MT);
-    const long long stride = (long long)gridDim.x * streams * (16 * MT);
-    if (n0 >= p.N || row0 >= rows) return;
-    const uint32_t wide = (uint32_t)min(16 * NT, p.N - n0);
-    const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.w + (size_t)n0 * p.pitch), 0, (int)(wide * p.pitch), kBufWord3);
+    long long row0 = ((long long)wave * gridDim.x + blockIdx.x) * (16 * MT);      // (few steps go to as many workgroups)
+    const long long stride = (long long)gridDim.x * kStreamWaves * (16 * MT);
+    if ((long long)blockIdx.x * (16 * MT) >= rows) return;
     uint32_t arel[MT], k[KC];
 #pragma unroll
     for (int i = 0; i < KC; ++i) k[i] = (uint32_t)(i * 64 + q * 16) < (uint32_t)p.pitch ? (uint32_t)(i * 64 + q * 16) : kOutOfRange;
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(256, 2) void i8_stream(PointArgs p, int groups, int
         float scale[MT];
     };
     auto load = [&](Rows &o, long long at) __attribute__((always_inline)) {
-        const uint32_t here = (uint32_t)min(16LL * MT, rows - at);
+        const uint32_t here = (uint32_t)max(0LL, min(16LL * MT, rows - at));
         const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a + (size_t)at * p.pitch), 0, (int)(here * p.pitch), kBufWord3);
         const __amdgpu_buffer_rsrc_t sr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a_scales + at), 0, (int)(here * 4), kBufWord3);
 #pragma unroll
@@ -429,53 +429,61 @@ __global__ __launch_bounds__(256, 2) void i8_stream(PointArgs p, int groups, int
             o.scale[m] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sr, (m * 16 + l16) * 4, 0, 0));
         }
     };
+    const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc((void *)p.w, 0, (int)((uint32_t)p.N * p.pitch), kBufWord3);
+    for (int f = wave; f < groups * KC * 4; f += kStreamWaves) {
+        const int g = f / (KC * 4), i = f / 4 % KC, n = f % 4;
+        const uint32_t at = (uint32_t)(i * 64 + q * 16), o = (uint32_t)(g * 64 + (n >> 1) * 32 + (l16 >> 2) * 8 + (n & 1) * 4 + (l16 & 3));
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(ldsb + f * 1024), 16, (int)(at < (uint32_t)p.pitch ? o * p.pitch + at : kOutOfRange), 0, 0, 0);
+    }
+    float *const sc = (float *)(lds + groups * KC * 4096);       // [groups][64] scales, then biases
+    for (int c = threadIdx.x; c < groups * 64; c += 64 * kStreamWaves) {
+        sc[c] = c < p.N ? p.w_scales[c] : 0.f;
+        sc[groups * 64 + c] = c < p.N && p.bias ? p.bias[c] : 0.f;
+    }
     Rows o0, o1;
     load(o0, row0);
-    uint4 w[NT][KC];
-    float ws[NT][4], bs[NT][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const uint32_t rel = (uint32_t)((n >> 1) * 32 + (l16 >> 2) * 8 + (n & 1) * 4 + (l16 & 3)) * p.pitch;
-#pragma unroll
-        for (int i = 0; i < KC; ++i) w[n][i] = buf_load16(wr, rel + k[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int c = n0 + (n >> 1) * 32 + q * 8 + (n & 1) * 4 + e;
-            ws[n][e] = c < p.N ? p.w_scales[c] : 0.f;
-            bs[n][e] = c < p.N && p.bias ? p.bias[c] : 0.f;
-        }
-    }
+    __syncthreads();
     auto step = [&](const Rows &o, long long at) __attribute__((always_inline)) {
+        for (int g = 0; g < groups; ++g) {
+            const lds_byte *wf = ldsb + g * KC * 4096 + lane * 16;
+            i32x4 acc[MT][4];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            i32x4 acc[NT];
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) acc[n] = (i32x4){0, 0, 0, 0};
+                for (int n = 0; n < 4; ++n) acc[m][n] = (i32x4){0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < KC; ++i)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) acc[n] = mfma_i8_16(w[n][i], o.a[m][i], acc[n]);
-            const long long row = at + m * 16 + l16;
+                for (int n = 0; n < 4; ++n) {
+                    const uint4 w = read16(wf + (i * 4 + n) * 1024);
 #pragma unroll
-            for (int s = 0; s < NT / 2; ++s) {
-                float v[8];
+                    for (int m = 0; m < MT; ++m) acc[m][n] = mfma_i8_16(w, o.a[m][i], acc[m][n]);
+                }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = finish(acc[2 * s + (e >> 2)][e & 3], o.scale[m], ws[2 * s + (e >> 2)][e & 3], bs[2 * s + (e >> 2)][e & 3], p.relu);
-                const int c = n0 + s * 32 + q * 8;
-                if (row < rows) store8<DT>(p.out, (size_t)row * p.N + c, v, p.N - c, p.wide && c + 8 <= p.N);
+            for (int s = 0; s < 2; ++s) {
+                const int c = g * 64 + s * 32 + q * 8;
+                if (c >= p.N) continue;
+                float ws[8], bs[8];
+                load_floats<8>(ws, sc, c);
+                load_floats<8>(bs, sc + groups * 64, c);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const long long row = at + m * 16 + l16;
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = finish(acc[m][2 * s + (e >> 2)][e & 3], o.scale[m], ws[e], bs[e], p.relu);
+                    if (row < rows) store8<DT>(p.out, (size_t)row * p.N + c, v, p.N - c, p.wide && c + 8 <= p.N);
+                }
             }
         }
     };
-    for (;;) {
-        const bool more = row0 + stride < rows;
-        if (more) load(o1, row0 + stride);
+    while (row0 < rows) {
+        load(o1, row0 + stride);
         step(o0, row0);
-        if (!more) break;
         row0 += stride;
-        const bool again = row0 + stride < rows;
-        if (again) load(o0, row0 + stride);
+        if (row0 >= rows) break;
+        load(o0, row0 + stride);
         step(o1, row0);
-        if (!again) break;
         row0 += stride;
     }
 }
@@ -499,23 +507,29 @@ sbnet_status direct_go(const char *who, const PointArgs &p, long long rows, hipS
     return launch_status(who);
 }
 
-template <int DT, int KC, int NT, int MT>
+size_t stream_lds(int KC, int N) {
+    const size_t groups = (N + 63) / 64;
+    return groups * (KC * 4096 + 512);
+}
+template <int DT, int KC, int MT>
 sbnet_status stream_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
-    const int all = (p.N + 16 * NT - 1) / (16 * NT), gy = (all + 3) / 4, groups = (all + gy - 1) / gy, streams = 4 / groups;
-    const long long steps = (rows + 16 * MT * streams - 1) / (16 * MT * streams);
-    const int most = 512 / gy > 1 ? 512 / gy : 1;
-    hipLaunchKernelGGL((i8_stream<DT, KC, NT, MT>), dim3((unsigned)(steps < most ? steps : most), gy), dim3(64 * groups * streams), 0, s, p, groups, streams);
+    const long long steps = (rows + 16 * MT - 1) / (16 * MT);
+    const size_t lds = stream_lds(KC, p.N);
+    (void)hipFuncSetAttribute((const void *)i8_stream<DT, KC, MT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    hipLaunchKernelGGL((i8_stream<DT, KC, MT>), dim3((unsigned)(steps < 256 ? steps : 256)), dim3(64 * kStreamWaves), lds, s, p, (p.N + 63) / 64);
     return launch_status(who);
 }
 
 template <int DT>
 sbnet_status pointwise_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
-    if (p.pitch <= 512 && p.N <= 512 && rows >= 8192) {
-        if (p.pitch <= 64) return stream_go<DT, 1, 4, 4>(who, p, rows, s);
-        if (p.pitch <= 128) return stream_go<DT, 2, 4, 4>(who, p, rows, s);
-        if (p.pitch <= 256) return stream_go<DT, 4, 4, 2>(who, p, rows, s);
-        if (p.pitch <= 384) return stream_go<DT, 6, 2, 2>(who, p, rows, s);
-        return stream_go<DT, 8, 2, 2>(who, p, rows, s);
+    const int KC = (p.pitch + 63) / 64;
+    if (KC <= 8 && stream_lds(KC <= 4 ? KC : KC <= 6 ? 6 : 8, p.N) <= 160 * 1024 && rows >= 8192) {
+        if (KC == 1) return stream_go<DT, 1, 2>(who, p, rows, s);
+        if (KC == 2) return stream_go<DT, 2, 2>(who, p, rows, s);
+        if (KC == 3) return stream_go<DT, 3, 2>(who, p, rows, s);
+        if (KC == 4) return stream_go<DT, 4, 2>(who, p, rows, s);
+        if (KC <= 6) return stream_go<DT, 6, 2>(who, p, rows, s);
+        return stream_go<DT, 8, 2>(who, p, rows, s);
     }
     if (rows * p.N >= 256LL * 256 * 128) return tiles_go<DT, 2, 2, 4, 2>(who, p, rows, s);
     if (rows * p.N >= 64 * 128 * 128) return tiles_go<DT, 2, 2, 2, 2>(who, p, rows, s);
