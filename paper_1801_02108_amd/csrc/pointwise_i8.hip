@@ -31,23 +31,23 @@ struct PointArgs {
     const float *a_scales, *w_scales, *bias;
     const int32_t *count;
     void *out;
-    int cap, pixels, pitch, N, relu;
+    float least;
+    int cap, pixels, pitch, N;
     int wide;                    // rows of out start at multiples of 16 bytes
 };
 
-__device__ __forceinline__ float finish(int acc, float a_scale, float w_scale, float bias, int relu) {
+// The result of a sum; `least` is 0 with a ReLU, else -infinity.  (A NaN stays one.)
+__device__ __forceinline__ float finish(int acc, float a_scale, float w_scale, float bias, float least) {
 #pragma clang fp contract(off)
-    float v = (float)acc * a_scale;
-    v = v * w_scale;
-    v = v + bias;
-    return relu && v < 0.f ? 0.f : v;             // (a NaN stays one)
+    const float v = (float)acc * a_scale;
+    return __builtin_elementwise_maximum(fmaf(v, w_scale, bias), least);
 }
 
 // ---- large products: tiles of BM rows x BN channels through LDS ----------------------------------------------------------
 // 32 x 32 x 32 steps of the matrix unit: its first operand is the weights (32 channels), its second the activations (32 rows), 16 bytes of
 // codes per lane each, so that a lane's 16 sums are channels of one row.  In LDS both operands are rows of 128 bytes, piece q of row i
 // at place q ^ (i / 2 % 8): the 16-byte reads of 16 neighbouring rows fall on different banks.  Row i of 32 weight rows is channel
-// 16 (i / 4 % 2) + 4 (i / 8) + i % 4, which makes a lane's sums 16 neighbouring channels.
+// 16 (i / 16) + 8 (i / 4 % 2) + 4 (i / 8 % 2) + i % 4, which makes a lane's sums two times 8 neighbouring channels, next to the other half's.
 typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
 typedef __attribute__((__vector_size__(16 * sizeof(int)))) int i32x16;
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
@@ -60,25 +60,22 @@ __device__ __forceinline__ uint4 read16(const lds_byte *p) {
     const u32x4 v = *(const __attribute__((address_space(3))) u32x4 *)p;
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
-__device__ __forceinline__ int channel_of_row(int i) { return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3); }
+__device__ __forceinline__ int channel_of_row(int i) { return (i & 16) + 8 * ((i >> 2) & 1) + 4 * ((i >> 3) & 1) + (i & 3); }
 
-// the results of 16 neighbouring channels of one row; `wide`: they all exist and 16-byte stores fit
+// the results of 8 neighbouring channels of one row; `wide`: they all exist and 16-byte stores fit
 template <int DT>
-__device__ __forceinline__ void store16(void *out, size_t at, const float *v, int left, bool wide) {
+__device__ __forceinline__ void store8(void *out, size_t at, const float *v, int left, bool wide) {
     typedef typename Elem<DT>::T T;
     if (wide) {
         if (DT == SBNET_F32) {
-#pragma unroll
-            for (int k = 0; k < 16; k += 4) *(float4 *)((T *)out + at + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+            *(float4 *)((T *)out + at) = make_float4(v[0], v[1], v[2], v[3]);
+            *(float4 *)((T *)out + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
         } else {
-#pragma unroll
-            for (int k = 0; k < 16; k += 8)
-                *(uint4 *)((T *)out + at + k) = make_uint4(pack2<DT>(v[k], v[k + 1]), pack2<DT>(v[k + 2], v[k + 3]), pack2<DT>(v[k + 4], v[k + 5]),
-                                                           pack2<DT>(v[k + 6], v[k + 7]));
+            *(uint4 *)((T *)out + at) = make_uint4(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]), pack2<DT>(v[4], v[5]), pack2<DT>(v[6], v[7]));
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < 16; ++k)
+        for (int k = 0; k < 8; ++k)
             if (k < left) Elem<DT>::store((T *)out + at + k, v[k]);
     }
 }
@@ -236,21 +233,28 @@ void i8_tiles(PointArgs p) {
             int n0;
             tile_at(j, row0, n0);
             const float *sc = (const float *)(lds + 3 * kStage + (j & 3) * kScales);
+float as[MF];
 #pragma unroll
-            for (int m = 0; m < MF; ++m) {
-                const int r = (wm * MF + m) * 32 + l32;
-                const float as = sc[r];
-                const bool there = row0 + r < rows;
-                const size_t to = (size_t)(row0 + r) * p.N;
+            for (int m = 0; m < MF; ++m) as[m] = sc[(wm * MF + m) * 32 + l32];
 #pragma unroll
-                for (int n = 0; n < NF; ++n) {
-                    const int c = (wn * NF + n) * 32 + 16 * h;
-                    float v[16];
+            for (int n = 0; n < NF; ++n)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) v[e] = finish(acc[m][n][e], as, sc[BM + c + e], sc[BM + BN + c + e], p.relu);
-                    if (there) store16<DT>(p.out, to + n0 + c, v, p.N - n0 - c, p.wide && n0 + c + 16 <= p.N);
+                for (int g = 0; g < 2; ++g) {
+                    const int c = (wn * NF + n) * 32 + 16 * g + 8 * h;
+                    if (n0 + c >= p.N) continue;
+                    float ws[8], bs[8];
+                    load_floats<8>(ws, sc + BM, c);
+                    load_floats<8>(bs, sc + BM + BN, c);
+                    const bool wide = p.wide && n0 + c + 8 <= p.N;
+#pragma unroll
+                    for (int m = 0; m < MF; ++m) {
+                        const long long row = row0 + (wm * MF + m) * 32 + l32;
+                        float v[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = finish(acc[m][n][8 * g + e], as[m], ws[e], bs[e], p.least);
+                        if (row < rows) store8<DT>(p.out, (size_t)row * p.N + n0 + c, v, p.N - n0 - c, wide);
+                    }
                 }
-            }
         }
     }
 }
@@ -369,8 +373,8 @@ __global__ __launch_bounds__(64 * KS) void i8_direct(PointArgs p) {
             t.x += u.x; t.y += u.y; t.z += u.z; t.w += u.w;
         }
         const int r = m * 16 + l16, c = n0 + 4 * NT * q + 4 * n;
-        const float v[4] = {finish(t.x, as[i], ws[i][0], bs[i][0], p.relu), finish(t.y, as[i], ws[i][1], bs[i][1], p.relu),
-                            finish(t.z, as[i], ws[i][2], bs[i][2], p.relu), finish(t.w, as[i], ws[i][3], bs[i][3], p.relu)};
+        const float v[4] = {finish(t.x, as[i], ws[i][0], bs[i][0], p.least), finish(t.y, as[i], ws[i][1], bs[i][1], p.least),
+                            finish(t.z, as[i], ws[i][2], bs[i][2], p.least), finish(t.w, as[i], ws[i][3], bs[i][3], p.least)};
         if ((uint32_t)r < here) store4<DT>(p.out, (size_t)(row0 + r) * p.N + c, v, p.N - c, p.wide && c + 4 <= p.N);
     }
 }
@@ -380,23 +384,6 @@ __global__ __launch_bounds__(64 * KS) void i8_direct(PointArgs p) {
 // and 2 s + 1 hold channels 32 s + 8 q + 4 (n % 2) + r in their rows 4 q + r: a lane's pair is 8 neighbouring channels, and one 16-byte store of
 // a wave is 64 bytes of each of 16 rows.
 // Bound by memory: the next step's rows are requested before this one's are multiplied.
-template <int DT>
-__device__ __forceinline__ void store8(void *out, size_t at, const float *v, int left, bool wide) {
-    typedef typename Elem<DT>::T T;
-    if (wide) {
-        if (DT == SBNET_F32) {
-            *(float4 *)((T *)out + at) = make_float4(v[0], v[1], v[2], v[3]);
-            *(float4 *)((T *)out + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            *(uint4 *)((T *)out + at) = make_uint4(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]), pack2<DT>(v[4], v[5]), pack2<DT>(v[6], v[7]));
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < left) Elem<DT>::store((T *)out + at + k, v[k]);
-    }
-}
-
 constexpr int kStreamWaves = 8;
 
 template <int DT, int KC, int MT>
@@ -471,7 +458,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void i8_stream(PointArgs p, i
                     const long long row = at + m * 16 + l16;
                     float v[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = finish(acc[m][2 * s + (e >> 2)][e & 3], o.scale[m], ws[e], bs[e], p.relu);
+                    for (int e = 0; e < 8; ++e) v[e] = finish(acc[m][2 * s + (e >> 2)][e & 3], o.scale[m], ws[e], bs[e], p.least);
                     if (row < rows) store8<DT>(p.out, (size_t)row * p.N + c, v, p.N - c, p.wide && c + 8 <= p.N);
                 }
             }
@@ -589,7 +576,7 @@ extern "C" sbnet_status sbnet_pointwise_i8_on_tiles(const int8_t *codes, const f
     if (cap == 0) return SBNET_OK;
     PointArgs p = {};
     p.a = codes; p.w = w_codes; p.a_scales = scales; p.w_scales = w_scales; p.bias = bias; p.count = count; p.out = out;
-    p.cap = cap; p.pixels = pixels; p.pitch = pitch; p.N = Cout; p.relu = relu ? 1 : 0;
+    p.cap = cap; p.pixels = pixels; p.pitch = pitch; p.N = Cout; p.least = relu ? 0.f : -INFINITY;
     p.wide = (long long)Cout * elem_bytes(dtype) % 16 == 0;
     hipStream_t s = (hipStream_t)stream;
     if (dtype == SBNET_F32) return pointwise_go<SBNET_F32>(who, p, (long long)rows, s);
