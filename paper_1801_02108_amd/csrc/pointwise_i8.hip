@@ -507,10 +507,44 @@ sbnet_status stream_go(const char *who, const PointArgs &p, long long rows, hipS
     return launch_status(who);
 }
 
+// What a shape of work costs: `channel` ns for each channel summed over and `result` ns at the end, times the rounds of 256 workgroups.  Fitted to 210 products of
+// 1 .. 100000 rows and 32 .. 8192 channels on either side, where the smallest estimate is mostly the fastest of the eight or within a tenth of it.
+// E.g. (us) 16 x 4096 x 4096: 6.8 with 16 x 16 a workgroup, 9.1 with 32 x 32, 10.9 with 64 x 64; 64 rows: 14.0, 10.7, 11.3; 128: 17.8
+// with 32 x 32, 11.8 with 64 x 64, 13.0 with 64 x 128; 512: 20.6, 15.4 and, with 128 x 128, 17.6; 1024: 28, 21.9 with 128 x 128, 27.6
+// with 256 x 128; 2048: 39 and 36.5; 256 x 512 x 512: 4.7 with 32 x 32, 5.3 with 64 x 64.
+struct Shape {
+    int rows, channels;
+    float channel, result;
+};
+constexpr Shape kShapes[] = {{16, 16, 0.95f, 500}, {16, 32, 1.4f, 600}, {32, 16, 1.4f, 600}, {32, 32, 1.85f, 450},
+                             {64, 64, 2.0f, 800}, {64, 128, 2.35f, 1000}, {128, 128, 3.15f, 2000}, {256, 128, 5.4f, 4000}};
+
+int cheapest(long long rows, int N, int pitch) {
+    int best = 0;
+    float least = 0.f;
+    for (int i = 0; i < 8; ++i) {
+        const Shape &s = kShapes[i];
+        const long long tiles = ((rows + s.rows - 1) / s.rows) * (((long long)N + s.channels - 1) / s.channels);
+        const float cost = (float)((tiles + 255) / 256) * (s.channel * (float)pitch + s.result);
+        if (i == 0 || cost < least) {
+            best = i;
+            least = cost;
+        }
+    }
+    return best;
+}
+
+// Long lists whose weights fit LDS are streamed.  (us, streamed and the best of the others: 112640 x 256 x 64 11.4 and 12.5, 112640 x 64 x 256 14.4
+// and 21.8, 112640 x 256 x 256 21.8 and 24.2, 32768 x 64 x 256 8.2 and 9.8, 8192 x 256 x 64 4.9 and 4.9; but 8192 x 64 x 256 6.2 and 5.4, 32768 x
+// 256 x 256 11.6 and 10.6.)
+bool streams(long long rows, int N, int KC) {
+    return KC <= 8 && stream_lds(KC <= 4 ? KC : KC <= 6 ? 6 : 8, N) <= 160 * 1024 && rows >= (N <= 64 ? 8192 : KC * N <= 512 ? 24576 : 65536);
+}
+
 template <int DT>
 sbnet_status pointwise_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
     const int KC = (p.pitch + 63) / 64;
-    if (KC <= 8 && stream_lds(KC <= 4 ? KC : KC <= 6 ? 6 : 8, p.N) <= 160 * 1024 && rows >= 8192) {
+    if (streams(rows, p.N, KC)) {
         if (KC == 1) return stream_go<DT, 1, 2>(who, p, rows, s);
         if (KC == 2) return stream_go<DT, 2, 2>(who, p, rows, s);
         if (KC == 3) return stream_go<DT, 3, 2>(who, p, rows, s);
@@ -518,12 +552,16 @@ sbnet_status pointwise_go(const char *who, const PointArgs &p, long long rows, h
         if (KC <= 6) return stream_go<DT, 6, 2>(who, p, rows, s);
         return stream_go<DT, 8, 2>(who, p, rows, s);
     }
-    if (rows * p.N >= 256LL * 256 * 128) return tiles_go<DT, 2, 2, 4, 2>(who, p, rows, s);
-    if (rows * p.N >= 64 * 128 * 128) return tiles_go<DT, 2, 2, 2, 2>(who, p, rows, s);
-    if (rows <= 16) return direct_go<DT, 1, 1, 8>(who, p, rows, s);
-    if (rows <= 32) return direct_go<DT, 2, 1, 8>(who, p, rows, s);
-    if (rows <= 64) return direct_go<DT, 2, 2, 4>(who, p, rows, s);
-    return direct_go<DT, 4, 2, 4>(who, p, rows, s);
+    switch (cheapest(rows, p.N, p.pitch)) {
+        case 0: return direct_go<DT, 1, 1, 8>(who, p, rows, s);
+        case 1: return direct_go<DT, 1, 2, 8>(who, p, rows, s);
+        case 2: return direct_go<DT, 2, 1, 8>(who, p, rows, s);
+        case 3: return direct_go<DT, 2, 2, 4>(who, p, rows, s);
+        case 4: return tiles_go<DT, 2, 2, 1, 1>(who, p, rows, s);
+        case 5: return tiles_go<DT, 2, 2, 1, 2>(who, p, rows, s);
+        case 6: return tiles_go<DT, 2, 2, 2, 2>(who, p, rows, s);
+        default: return tiles_go<DT, 2, 2, 4, 2>(who, p, rows, s);
+    }
 }
 
 }  // namespace

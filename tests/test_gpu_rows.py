@@ -318,6 +318,8 @@ PRODUCTS = [
     # long lists of narrow layers
     (30, 324, 256, 64), (33, 256, 64, 250), (33, 256, 128, 130), (40, 256, 384, 96), (129, 64, 512, 40), (9001, 1, 16, 1), (36, 289, 80, 333),
     (41, 256, 320, 512), (128, 81, 448, 200), (33, 255, 32, 513),
+    # wide layers on long lists
+    (4099, 1, 208, 4104), (2047, 1, 1040, 8201), (41, 100, 528, 4113),
 ]
 
 
