@@ -26,8 +26,8 @@ struct RowArgs {
     int cap, pixels, C, pitch;
 };
 
-// T threads hold a row of up to T * P channels, E of them at a time; the workgroup has 256 threads or one row's.
-constexpr int wg_threads(int T) { return T < 256 ? 256 : T; }
+// T threads hold a row of up to T * P channels, E of them at a time; the workgroup has 256 threads or, where a wave does not hold a row, one row's.
+constexpr int wg_threads(int T) { return T <= 64 ? 256 : T; }
 
 template <int DT, int E, int T, int P, int FORM>
 __global__ __launch_bounds__(wg_threads(T)) void rms_rows(RowArgs p) {
@@ -169,8 +169,7 @@ __global__ __launch_bounds__(wg_threads(T)) void rms_backward_rows(BackArgs p) {
             ss += a * a;
             gs += gain[k] * d[k / E].get(k % E) * a;
         }
-        ss = __uint_as_float(over_row<T>(__float_as_uint(ss), AddF32(), slots[turn][0]));
-        gs = __uint_as_float(over_row<T>(__float_as_uint(gs), AddF32(), slots[turn][1]));
+        over_row2<T>(ss, gs, slots[turn][0], slots[turn][1]);
         const float r = rsqrtf(ss * p.inv_c + p.eps), m = gs * p.inv_c * r;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -187,6 +186,7 @@ __global__ __launch_bounds__(wg_threads(T)) void rms_backward_rows(BackArgs p) {
         }
     }
     float *part = p.part + (size_t)blockIdx.x * p.C;
+    const bool quads = E >= 4 && ((uintptr_t)p.part & 15) == 0;
     if (RB > 1) {
 #pragma unroll
         for (int k = 0; k < P; ++k) sums[(threadIdx.x / T) * (T * P) + (k / E * T + t) * E + k % E] = dg[k];
@@ -199,9 +199,15 @@ __global__ __launch_bounds__(wg_threads(T)) void rms_backward_rows(BackArgs p) {
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
+        for (int k = 0; k < P; k += E >= 4 ? 4 : 1) {
             const int c = (k / E * T + t) * E + k % E;
-            if (c < p.C) part[c] = dg[k];
+            if (c >= p.C) continue;
+            if (quads) {
+                *(float4 *)(part + c) = make_float4(dg[k], dg[k + 1 < P ? k + 1 : k], dg[k + 2 < P ? k + 2 : k], dg[k + 3 < P ? k + 3 : k]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < (E >= 4 ? 4 : 1); ++e) part[c + e] = dg[k + e];
+            }
         }
     }
 }
@@ -247,10 +253,10 @@ void by_width(int C, F f) {
     else if (C <= 256) f(Split<32, 8>());
     else if (C <= 512) f(Split<64, 8>());
     else if (C <= 1024) f(Split<64, 16>());
-    else if (C <= 2048) f(Split<256, 8>());
+    else if (C <= 2048) f(Split<128, 16>());
     else if (C <= 4096) f(Split<256, 16>());
-    else if (C <= 8192) f(Split<1024, 8>());
-    else if (C <= 16384) f(Split<1024, 16>());
+    else if (C <= 8192) f(Split<512, 16>());
+    else if (C <= 16384) f(Split<512, 32>());
     else f(Split<1024, 32>());
 }
 
@@ -260,10 +266,13 @@ int back_grid(long long rows, int C) {
     by_width(C, [&](auto w) {
         constexpr int T = decltype(w)::T;
         rb = wg_threads(T) / T;
-        most = T > 256 ? 512 : 1024;
+        most = wg_threads(T) > 256 ? 256 : 131072 / wg_threads(T);
     });
     const long long want = (rows + rb - 1) / rb;
-    return (int)(want < most ? want : most);
+    if (want <= 3) return want > 0 ? 1 : 0;       // a few rows one after the other end sooner than a second launch
+    if (want <= 128) return (int)want;
+    const long long half = want / 2 > 128 ? (want + 1) / 2 : 128;
+    return (int)(half < most ? half : most);
 }
 
 sbnet_status check_rows(const char *who, sbnet_dtype dtype, int cap, int pixels, int C, int most) {
@@ -397,17 +406,18 @@ extern "C" sbnet_status sbnet_rms_norm_backward_on_tiles(const void *s, const vo
             return fail(SBNET_EINVAL, "%s: stacks overlap", who);
     if (ranges_overlap(dgain, (size_t)C * 4, workspace, need)) return fail(SBNET_EINVAL, "%s: workspace overlaps dgain", who);
     BackArgs p = {};
-    p.s = s; p.dy = dy; p.dsum = dsum; p.dx = dx; p.gain = gain; p.part = (float *)workspace; p.count = count;
+    p.s = s; p.dy = dy; p.dsum = dsum; p.dx = dx; p.gain = gain; p.count = count;
     p.eps = eps; p.inv_c = 1.f / (float)C; p.cap = cap; p.pixels = pixels; p.C = C;
     const int grid = back_grid((long long)cap * pixels, C);
     const bool wide = (size_t)C * es % 16 == 0 && (stacks | (uintptr_t)gain) % 16 == 0;
+    p.part = grid == 1 ? dgain : (float *)workspace;              // (one workgroup's sums are the result)
     hipStream_t q = (hipStream_t)stream;
     if (grid > 0) {
         if (dtype == SBNET_F32) back_form<SBNET_F32>(wide, p, grid, q);
         else if (dtype == SBNET_BF16) back_form<SBNET_BF16>(wide, p, grid, q);
         else back_form<SBNET_F16>(wide, p, grid, q);
         const sbnet_status done = launch_status(who);
-        if (done != SBNET_OK) return done;
+        if (done != SBNET_OK || grid == 1) return done;
     }
     hipLaunchKernelGGL(rms_dgain_sum, dim3((C + 63) / 64), dim3(1024), 0, q, p.part, grid, C, dgain);
     return launch_status(who);

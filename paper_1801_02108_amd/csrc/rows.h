@@ -88,6 +88,27 @@ __device__ __forceinline__ uint32_t over_row(uint32_t v, F f, uint32_t *slots) {
     return v;
 }
 
+// ... the sums of two numbers at once
+template <int T>
+__device__ __forceinline__ void over_row2(float &a, float &b, uint32_t *slots_a, uint32_t *slots_b) {
+    constexpr int L = T <= 64 ? T : 64;
+    a = __uint_as_float(over_lanes<L>(__float_as_uint(a), AddF32()));
+    b = __uint_as_float(over_lanes<L>(__float_as_uint(b), AddF32()));
+    if (T <= 64) return;
+    if ((threadIdx.x & 63) == 0) {
+        slots_a[threadIdx.x >> 6] = __float_as_uint(a);
+        slots_b[threadIdx.x >> 6] = __float_as_uint(b);
+    }
+    __syncthreads();
+    a = __uint_as_float(slots_a[0]);
+    b = __uint_as_float(slots_b[0]);
+#pragma unroll
+    for (int w = 1; w < T / 64; ++w) {
+        a += __uint_as_float(slots_a[w]);
+        b += __uint_as_float(slots_b[w]);
+    }
+}
+
 // E neighbouring elements of a row: 16 bytes, or one element where rows do not start at multiples of 16 bytes
 template <int DT, int E>
 struct Piece {
