@@ -62,6 +62,15 @@ __device__ __forceinline__ uint4 read16(const lds_byte *p) {
 }
 __device__ __forceinline__ int channel_of_row(int i) { return (i & 16) + 8 * ((i >> 2) & 1) + 4 * ((i >> 3) & 1) + (i & 3); }
 
+// 8 floats from LDS
+__device__ __forceinline__ void load8(float *v, const float *p) {
+#pragma unroll
+    for (int e = 0; e < 8; e += 4) {
+        const float4 q = *(const float4 *)(p + e);
+        v[e] = q.x; v[e + 1] = q.y; v[e + 2] = q.z; v[e + 3] = q.w;
+    }
+}
+
 // the results of 8 neighbouring channels of one row; `wide`: they all exist and 16-byte stores fit
 template <int DT>
 __device__ __forceinline__ void store8(void *out, size_t at, const float *v, int left, bool wide) {
@@ -243,8 +252,8 @@ float as[MF];
                     const int c = (wn * NF + n) * 32 + 16 * g + 8 * h;
                     if (n0 + c >= p.N) continue;
                     float ws[8], bs[8];
-                    load_floats<8>(ws, sc + BM, c);
-                    load_floats<8>(bs, sc + BM + BN, c);
+                    load8(ws, sc + BM + c);
+                    load8(bs, sc + BM + BN + c);
                     const bool wide = p.wide && n0 + c + 8 <= p.N;
 #pragma unroll
                     for (int m = 0; m < MF; ++m) {
@@ -451,8 +460,8 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void i8_stream(PointArgs p, i
                 const int c = g * 64 + s * 32 + q * 8;
                 if (c >= p.N) continue;
                 float ws[8], bs[8];
-                load_floats<8>(ws, sc, c);
-                load_floats<8>(bs, sc + groups * 64, c);
+                load8(ws, sc + c);
+                load8(bs, sc + groups * 64 + c);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     const long long row = at + m * 16 + l16;

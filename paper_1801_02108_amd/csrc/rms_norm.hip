@@ -29,38 +29,39 @@ struct RowArgs {
 // T threads hold a row of up to T * P channels, E of them at a time; the workgroup has 256 threads or, where a wave does not hold a row, one row's.
 constexpr int wg_threads(int T) { return T <= 64 ? 256 : T; }
 
-template <int DT, int E, int T, int P, int FORM>
+template <class V, int T, int P, int FORM>
 __global__ __launch_bounds__(wg_threads(T)) void rms_rows(RowArgs p) {
-    constexpr int NV = P / E, RB = wg_threads(T) / T;
+    constexpr int E = V::E, NV = P / E, RB = wg_threads(T) / T;
     __shared__ uint32_t slots[2][2][16];
     const long long rows = active_rows(p.count, p.cap, p.pixels);
     const int t = threadIdx.x % T;
+    const Span<SBNET_F32> gains(p.gain, 0, 1, p.C);
     float gain[P];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int c = (v * T + t) * E;
 #pragma unroll
         for (int e = 0; e < E; ++e) gain[v * E + e] = 1.f;
-        if (FORM != kCodes && p.gain && c < p.C) load_floats<E>(gain + v * E, p.gain, c);
+        if (FORM != kCodes && p.gain) load_floats<E>(gain + v * E, gains, c, p.C);
     }
     int turn = 0;
     for (long long first = (long long)blockIdx.x * RB; first < rows; first += (long long)gridDim.x * RB, turn ^= 1) {
         const long long row = first + threadIdx.x / T;
         if (T <= 64 && row >= rows) break;                        // (a workgroup of one row has no such thread)
-        const size_t at = (size_t)row * p.C;
-        Piece<DT, E> x[NV], res[NV];
+        const uint32_t at = threadIdx.x / T * p.C;                // of the rows from `first` on
+        const int here = (int)min((long long)RB, rows - first);
+        const Span<V::kType> xs(p.x, first, here, p.C), rs(p.res, first, here, p.C), sums(p.sum, first, here, p.C), ys(p.y, first, here, p.C);
+        V x[NV], res[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * T + t) * E;
-            x[v].clear();
-            if (c < p.C) x[v].load(p.x, at + c);
+            x[v].load(xs, at + c, p.C - c);
         }
         if (FORM != kCodes && p.res) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int c = (v * T + t) * E;
-                res[v].clear();
-                if (c < p.C) res[v].load(p.res, at + c);
+                res[v].load(rs, at + c, p.C - c);
             }
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
@@ -69,7 +70,7 @@ __global__ __launch_bounds__(wg_threads(T)) void rms_rows(RowArgs p) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) sum[e] = x[v].get(e) + res[v].get(e);
                 x[v].set(sum);
-                if (c < p.C) x[v].store(p.sum, at + c);
+                x[v].store(sums, at + c, p.C - c);
             }
         }
         float s[P];
@@ -89,7 +90,7 @@ __global__ __launch_bounds__(wg_threads(T)) void rms_rows(RowArgs p) {
             for (int v = 0; v < NV; ++v) {
                 const int c = (v * T + t) * E;
                 x[v].set(s + v * E);
-                if (c < p.C) x[v].store(p.y, at + c);
+                x[v].store(ys, at + c, p.C - c);
             }
         } else {
             uint32_t top = 0;
@@ -103,12 +104,9 @@ __global__ __launch_bounds__(wg_threads(T)) void rms_rows(RowArgs p) {
             for (int v = 0; v < NV; ++v) {
                 const int c = (v * T + t) * E;
                 if (c >= p.pitch) continue;
-                if (E == 1) {
-                    to[c] = code1(s[v], rc.inv, keep);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; e += 4) *(uint32_t *)(to + c + e) = codes4(s + v * E + e, rc.inv, keep);
-                }
+                if (E == 1) to[c] = code1(s[v], rc.inv, keep);
+                else if (E == 8) *(uint2 *)(to + c) = make_uint2(codes4(s + v * E, rc.inv, keep), codes4(s + v * E + (E == 8 ? 4 : 0), rc.inv, keep));
+                else *(uint32_t *)(to + c) = codes4(s + v * E, rc.inv, keep);
             }
             if (t == 0) p.scales[row] = rc.scale;
         }
@@ -125,68 +123,78 @@ struct BackArgs {
     int cap, pixels, C;
 };
 
-// A thread keeps its channels' sums of dy h over all its rows; the workgroup adds those of its rows' places in ascending order.
-template <int DT, int E, int T, int P>
+// A thread keeps its channels' sums of dy h over all its rows; the workgroup adds those of its rows' places in ascending order.  With 32 channels a
+// thread the gains, and the gradient past the norm until it is added, stay in memory: the registers hold no more.
+template <class V, int T, int P>
 __global__ __launch_bounds__(wg_threads(T)) void rms_backward_rows(BackArgs p) {
-    constexpr int NV = P / E, RB = wg_threads(T) / T;
+    constexpr int E = V::E, NV = P / E, RB = wg_threads(T) / T;
+    constexpr bool kKeep = P <= 16;
     __shared__ uint32_t slots[2][2][16];
     __shared__ float sums[RB > 1 ? RB * T * P : 1];
     const long long rows = active_rows(p.count, p.cap, p.pixels);
     const int t = threadIdx.x % T;
-    float gain[P], dg[P];
+    const Span<SBNET_F32> gains(p.gain, 0, 1, p.C);
+    float kept[kKeep ? P : 1], dg[P];
+    auto load_gain = [&](float *g, int v) __attribute__((always_inline)) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int c = (v * T + t) * E;
+        for (int e = 0; e < E; ++e) g[e] = 1.f;
+        if (p.gain) load_floats<E>(g, gains, (v * T + t) * E, p.C);
+    };
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            gain[v * E + e] = 1.f;
-            dg[v * E + e] = 0.f;
-        }
-        if (p.gain && c < p.C) load_floats<E>(gain + v * E, p.gain, c);
+    for (int k = 0; k < P; ++k) dg[k] = 0.f;
+    if (kKeep) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) load_gain(kept + (kKeep ? v * E : 0), v);
     }
     int turn = 0;
     for (long long first = (long long)blockIdx.x * RB; first < rows; first += (long long)gridDim.x * RB, turn ^= 1) {
         const long long row = first + threadIdx.x / T;
         if (T <= 64 && row >= rows) break;                        // (a workgroup of one row has no such thread)
-        const size_t at = (size_t)row * p.C;
-        Piece<DT, E> s[NV], d[NV], past[NV];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c = (v * T + t) * E;
-            s[v].clear();
-            d[v].clear();
-            past[v].clear();
-            if (c < p.C) {
-                s[v].load(p.s, at + c);
-                d[v].load(p.dy, at + c);
-                if (p.dsum) past[v].load(p.dsum, at + c);
-            }
-        }
+        const uint32_t at = threadIdx.x / T * p.C;                // of the rows from `first` on
+        const int here = (int)min((long long)RB, rows - first);
+        const Span<V::kType> xs(p.s, first, here, p.C), ds(p.dy, first, here, p.C), us(p.dsum, first, here, p.C), to(p.dx, first, here, p.C);
+        V s[NV], d[NV], past[kKeep ? NV : 1];
         float ss = 0.f, gs = 0.f;
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const float a = s[k / E].get(k % E);
-            ss += a * a;
-            gs += gain[k] * d[k / E].get(k % E) * a;
+        for (int v = 0; v < NV; ++v) s[v].load(xs, at + (v * T + t) * E, p.C - (v * T + t) * E);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) d[v].load(ds, at + (v * T + t) * E, p.C - (v * T + t) * E);
+        if (kKeep && p.dsum) {
+#pragma unroll
+            for (int v = 0; v < (kKeep ? NV : 1); ++v) past[v].load(us, at + (v * T + t) * E, p.C - (v * T + t) * E);
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float g[E];
+            if (!kKeep) load_gain(g, v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float a = s[v].get(e);
+                ss += a * a;
+                gs += (kKeep ? kept[kKeep ? v * E + e : 0] : g[e]) * d[v].get(e) * a;
+            }
         }
         over_row2<T>(ss, gs, slots[turn][0], slots[turn][1]);
         const float r = rsqrtf(ss * p.inv_c + p.eps), m = gs * p.inv_c * r;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * T + t) * E;
-            float dx[E];
+            V &q = past[kKeep ? v : 0];
+            if (!kKeep && p.dsum) q.load(us, at + c, p.C - c);
+            float g[E], dx[E];
+            if (!kKeep) load_gain(g, v);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const float h = s[v].get(e) * r, dy = d[v].get(e);
                 dg[v * E + e] += dy * h;
-                dx[e] = r * (gain[v * E + e] * dy - h * m) + past[v].get(e);
+                dx[e] = r * ((kKeep ? kept[kKeep ? v * E + e : 0] : g[e]) * dy - h * m);
+                if (p.dsum) dx[e] += q.get(e);
             }
             s[v].set(dx);
-            if (c < p.C) s[v].store(p.dx, at + c);
+            s[v].store(to, at + c, p.C - c);
         }
     }
     float *part = p.part + (size_t)blockIdx.x * p.C;
-    const bool quads = E >= 4 && ((uintptr_t)p.part & 15) == 0;
     if (RB > 1) {
 #pragma unroll
         for (int k = 0; k < P; ++k) sums[(threadIdx.x / T) * (T * P) + (k / E * T + t) * E + k % E] = dg[k];
@@ -199,14 +207,14 @@ __global__ __launch_bounds__(wg_threads(T)) void rms_backward_rows(BackArgs p) {
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < P; k += E >= 4 ? 4 : 1) {
+        for (int k = 0; k < P; k += E == 1 ? 1 : 4) {
             const int c = (k / E * T + t) * E + k % E;
-            if (c >= p.C) continue;
-            if (quads) {
-                *(float4 *)(part + c) = make_float4(dg[k], dg[k + 1 < P ? k + 1 : k], dg[k + 2 < P ? k + 2 : k], dg[k + 3 < P ? k + 3 : k]);
+            if (E == 1) {
+                if (c < p.C) part[c] = dg[k];
             } else {
-#pragma unroll
-                for (int e = 0; e < (E >= 4 ? 4 : 1); ++e) part[c + e] = dg[k + e];
+                Piece<SBNET_F32> q;
+                q.set(dg + k);
+                q.store(Span<SBNET_F32>(part, 0, 1, p.C), c, p.C - c);
             }
         }
     }
@@ -288,33 +296,33 @@ bool clash(const void *a, const void *b, size_t bytes) { return a && b && a != b
 
 bool eps_ok(float eps) { return eps > 0.f && eps * 0.f == 0.f; }
 
-template <int DT, int E>
-void rows_width(Form form, const RowArgs &p, size_t rows, hipStream_t s) {
+template <class V>
+void rows_as(Form form, const RowArgs &p, size_t rows, hipStream_t s) {
     by_width(form == kNorm ? p.C : p.pitch, [&](auto w) {         // (the codes fill the padding too)
         constexpr int T = decltype(w)::T, P = decltype(w)::P, RB = wg_threads(T) / T;
         const size_t want = (rows + RB - 1) / RB;
         const int grid = (int)(want < 4096 ? want : 4096);
-        if (form == kNorm) hipLaunchKernelGGL((rms_rows<DT, E, T, P, kNorm>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
-        else if (form == kNormCodes) hipLaunchKernelGGL((rms_rows<DT, E, T, P, kNormCodes>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
-        else hipLaunchKernelGGL((rms_rows<DT, E, T, P, kCodes>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
+        if (form == kNorm) hipLaunchKernelGGL((rms_rows<V, T, P, kNorm>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
+        else if (form == kNormCodes) hipLaunchKernelGGL((rms_rows<V, T, P, kNormCodes>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
+        else hipLaunchKernelGGL((rms_rows<V, T, P, kCodes>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
     });
 }
-template <int DT>
-void rows_form(Form form, bool wide, const RowArgs &p, size_t rows, hipStream_t s) {
-    if (wide) rows_width<DT, DT == SBNET_F32 ? 4 : 8>(form, p, rows, s);
-    else rows_width<DT, 1>(form, p, rows, s);
-}
-template <int DT, int E>
-void back_width(const BackArgs &p, int grid, hipStream_t s) {
+template <class V>
+void back_as(const BackArgs &p, int grid, hipStream_t s) {
     by_width(p.C, [&](auto w) {
         constexpr int T = decltype(w)::T, P = decltype(w)::P;
-        hipLaunchKernelGGL((rms_backward_rows<DT, E, T, P>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
+        hipLaunchKernelGGL((rms_backward_rows<V, T, P>), dim3(grid), dim3(wg_threads(T)), 0, s, p);
     });
 }
 template <int DT>
-void back_form(bool wide, const BackArgs &p, int grid, hipStream_t s) {
-    if (wide) back_width<DT, DT == SBNET_F32 ? 4 : 8>(p, grid, s);
-    else back_width<DT, 1>(p, grid, s);
+void rows_go(Form form, bool wide, const RowArgs &p, size_t rows, hipStream_t s) {
+    if (wide) rows_as<Piece<DT>>(form, p, rows, s);
+    else rows_as<Single<DT>>(form, p, rows, s);
+}
+template <int DT>
+void back_go(bool wide, const BackArgs &p, int grid, hipStream_t s) {
+    if (wide) back_as<Piece<DT>>(p, grid, s);
+    else back_as<Single<DT>>(p, grid, s);
 }
 
 sbnet_status rows_launch(const char *who, Form form, const void *x, const void *residual, sbnet_dtype dtype, const int32_t *count,
@@ -345,12 +353,12 @@ sbnet_status rows_launch(const char *who, Form form, const void *x, const void *
     RowArgs p = {};
     p.x = x; p.res = residual; p.sum = sum; p.y = y; p.codes = codes; p.scales = scales; p.gain = gain; p.count = count;
     p.eps = eps; p.inv_c = 1.f / (float)C; p.cap = cap; p.pixels = pixels; p.C = C; p.pitch = pitch;
-    const uintptr_t all = stacks | (uintptr_t)codes | (uintptr_t)gain;
-    const bool wide = (size_t)C * es % 16 == 0 && all % 16 == 0;
+    // 16-byte accesses where all rows start at multiples of 16 bytes
+    const bool wide = ((size_t)C * es | stacks | (uintptr_t)codes | (uintptr_t)gain) % 16 == 0;
     hipStream_t q = (hipStream_t)stream;
-    if (dtype == SBNET_F32) rows_form<SBNET_F32>(form, wide, p, rows, q);
-    else if (dtype == SBNET_BF16) rows_form<SBNET_BF16>(form, wide, p, rows, q);
-    else rows_form<SBNET_F16>(form, wide, p, rows, q);
+    if (dtype == SBNET_F32) rows_go<SBNET_F32>(form, wide, p, rows, q);
+    else if (dtype == SBNET_BF16) rows_go<SBNET_BF16>(form, wide, p, rows, q);
+    else rows_go<SBNET_F16>(form, wide, p, rows, q);
     return launch_status(who);
 }
 
@@ -409,13 +417,13 @@ extern "C" sbnet_status sbnet_rms_norm_backward_on_tiles(const void *s, const vo
     p.s = s; p.dy = dy; p.dsum = dsum; p.dx = dx; p.gain = gain; p.count = count;
     p.eps = eps; p.inv_c = 1.f / (float)C; p.cap = cap; p.pixels = pixels; p.C = C;
     const int grid = back_grid((long long)cap * pixels, C);
-    const bool wide = (size_t)C * es % 16 == 0 && (stacks | (uintptr_t)gain) % 16 == 0;
+    const bool wide = ((size_t)C * es | stacks | (uintptr_t)gain | (uintptr_t)workspace | (uintptr_t)dgain) % 16 == 0;
     p.part = grid == 1 ? dgain : (float *)workspace;              // (one workgroup's sums are the result)
     hipStream_t q = (hipStream_t)stream;
     if (grid > 0) {
-        if (dtype == SBNET_F32) back_form<SBNET_F32>(wide, p, grid, q);
-        else if (dtype == SBNET_BF16) back_form<SBNET_BF16>(wide, p, grid, q);
-        else back_form<SBNET_F16>(wide, p, grid, q);
+        if (dtype == SBNET_F32) back_go<SBNET_F32>(wide, p, grid, q);
+        else if (dtype == SBNET_BF16) back_go<SBNET_BF16>(wide, p, grid, q);
+        else back_go<SBNET_F16>(wide, p, grid, q);
         const sbnet_status done = launch_status(who);
         if (done != SBNET_OK || grid == 1) return done;
     }

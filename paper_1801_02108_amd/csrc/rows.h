@@ -109,54 +109,75 @@ __device__ __forceinline__ void over_row2(float &a, float &b, uint32_t *slots_a,
     }
 }
 
-// E neighbouring elements of a row: 16 bytes, or one element where rows do not start at multiples of 16 bytes
-template <int DT, int E>
-struct Piece {
-    static constexpr int kWords = E == 1 ? 1 : 4;
-    uint32_t w[kWords];
-    __device__ __forceinline__ void load(const void *p, size_t i) {
-        if (E > 1) {
-            const uint4 q = *(const uint4 *)((const typename Elem<DT>::T *)p + i);
-            w[0] = q.x; w[kWords > 1 ? 1 : 0] = q.y; w[kWords > 2 ? 2 : 0] = q.z; w[kWords > 3 ? 3 : 0] = q.w;
-        } else if (DT == SBNET_F32) {
-            w[0] = ((const uint32_t *)p)[i];
-        } else {
-            w[0] = ((const uint16_t *)p)[i];
-        }
+// The rows of a stack that a workgroup has before it: `rows` of them from row `first` on.  What lies behind a row's end is addressed out of the
+// buffer's range, which gives zeros and stores nothing without a branch.
+template <int DT>
+struct Span {
+    __amdgpu_buffer_rsrc_t r;
+    __device__ __forceinline__ Span(const void *stack, long long first, int rows, int C) {
+        constexpr int es = DT == SBNET_F32 ? 4 : 2;
+        r = __builtin_amdgcn_make_buffer_rsrc((char *)stack + (size_t)first * C * es, 0, stack ? rows * C * es : 0, kBufWord3);
     }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int k = 0; k < kWords; ++k) w[k] = 0;
+    // place of element i of the span, `left` of them before the row's end
+    static __device__ __forceinline__ uint32_t place(uint32_t i, int left) { return left > 0 ? i * (DT == SBNET_F32 ? 4u : 2u) : kOutOfRange; }
+};
+
+// 16 neighbouring bytes of a row, for rows that start at multiples of 16 bytes
+template <int DT>
+struct Piece {
+    static constexpr int kType = DT, E = DT == SBNET_F32 ? 4 : 8; // elements
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const Span<DT> &s, uint32_t i, int left) {
+        const uint4 q = buf_load16(s.r, Span<DT>::place(i, left));
+        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+    }
+    __device__ __forceinline__ void store(const Span<DT> &s, uint32_t i, int left) const {
+        const u32x4 v = {w[0], w[1], w[2], w[3]};
+        __builtin_amdgcn_raw_buffer_store_b128(v, s.r, (int)Span<DT>::place(i, left), 0, 0);
     }
     __device__ __forceinline__ float get(int e) const {
         if (DT == SBNET_F32) return __uint_as_float(w[e]);
         return e & 1 ? unpack_hi<DT>(w[e >> 1]) : unpack_lo<DT>(w[e >> 1]);
     }
     __device__ __forceinline__ void set(const float *v) {         // rounds to the type
-        if (DT == SBNET_F32) {
 #pragma unroll
-            for (int k = 0; k < kWords; ++k) w[k] = __float_as_uint(v[k]);
-        } else if (E == 1) {
-            w[0] = pack2<DT>(v[0], 0.f);
-        } else {
-#pragma unroll
-            for (int k = 0; k < kWords; ++k) w[k] = pack2<DT>(v[2 * k], v[E > 1 ? 2 * k + 1 : 0]);
-        }
-    }
-    __device__ __forceinline__ void store(void *p, size_t i) const {
-        if (E > 1) *(uint4 *)((typename Elem<DT>::T *)p + i) = make_uint4(w[0], w[kWords > 1 ? 1 : 0], w[kWords > 2 ? 2 : 0], w[kWords > 3 ? 3 : 0]);
-        else if (DT == SBNET_F32) ((uint32_t *)p)[i] = w[0];
-        else ((uint16_t *)p)[i] = (uint16_t)w[0];
+        for (int k = 0; k < 4; ++k) w[k] = DT == SBNET_F32 ? __float_as_uint(v[k]) : pack2<DT>(v[(2 * k) % E], v[(2 * k + 1) % E]);
     }
 };
-// ... of a float32 vector
+
+// one element, for the others (16-byte accesses at any address do work, at a lower rate than these: gradients of 28000 rows of 1004 f16 49 us with them, 38
+// so).  It is kept as it was loaded: converted at once, every load would be waited for.
+template <int DT>
+struct Single {
+    static constexpr int kType = DT, E = 1;
+    uint32_t w;
+    __device__ __forceinline__ void load(const Span<DT> &s, uint32_t i, int left) {
+        const int at = (int)Span<DT>::place(i, left);
+        w = DT == SBNET_F32 ? __builtin_amdgcn_raw_buffer_load_b32(s.r, at, 0, 0) : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(s.r, at, 0, 0);
+    }
+    __device__ __forceinline__ void store(const Span<DT> &s, uint32_t i, int left) const {
+        const int at = (int)Span<DT>::place(i, left);
+        if (DT == SBNET_F32) __builtin_amdgcn_raw_buffer_store_b32(w, s.r, at, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b16((unsigned short)w, s.r, at, 0, 0);
+    }
+    __device__ __forceinline__ float get(int) const { return DT == SBNET_F32 ? __uint_as_float(w) : unpack_lo<DT>(w); }
+    __device__ __forceinline__ void set(const float *f) { w = DT == SBNET_F32 ? __float_as_uint(f[0]) : pack2<DT>(f[0], 0.f); }
+};
+
+// E neighbouring floats of a vector of n, zeros behind it; with E > 1 n is a multiple of 4
 template <int E>
-__device__ __forceinline__ void load_floats(float *v, const float *p, int i) {
+__device__ __forceinline__ void load_floats(float *v, const Span<SBNET_F32> &s, int i, int n) {
+    if (E == 1) {
+        Single<SBNET_F32> q;
+        q.load(s, i, n - i);
+        v[0] = q.get(0);
+    } else {
 #pragma unroll
-    for (int e = 0; e < E; e += 4) {
-        if (E == 1) { v[0] = p[i]; break; }
-        const float4 q = *(const float4 *)(p + i + e);
-        v[e] = q.x; v[E > 1 ? e + 1 : 0] = q.y; v[E > 1 ? e + 2 : 0] = q.z; v[E > 1 ? e + 3 : 0] = q.w;
+        for (int e = 0; e < E; e += 4) {
+            Piece<SBNET_F32> q;
+            q.load(s, i + e, n - i - e);
+            v[e] = q.get(0); v[E > 1 ? e + 1 : 0] = q.get(1); v[E > 1 ? e + 2 : 0] = q.get(2); v[E > 1 ? e + 3 : 0] = q.get(3);
+        }
     }
 }
 
