@@ -388,42 +388,38 @@ __global__ __launch_bounds__(64 * KS) void i8_direct(PointArgs p) {
     }
 }
 
-// ---- long lists, few weights: all weights lie in LDS, every wave streams rows past them, 16 MT at a time
+// ---- long lists, few weights: all weights lie in LDS, every wave streams rows past them, 16 at a time
 // 16 x 16 x 64 steps on 64 channels at a time.  The weights are laid out in LDS as the operand reads take them, 1 KB each, once a workgroup.  Frags 2 s
 // and 2 s + 1 hold channels 32 s + 8 q + 4 (n % 2) + r in their rows 4 q + r: a lane's pair is 8 neighbouring channels, and one 16-byte store of
 // a wave is 64 bytes of each of 16 rows.
-// Bound by memory: the next step's rows are requested before this one's are multiplied.
-constexpr int kStreamWaves = 8;
+// Bound by memory: the next 16 rows are requested before these are multiplied, by twelve waves a CU (eight waves of 32 rows: 112640 x 256 x 256
+// 22.0 us instead of 20.2, 142560 x 256 x 64 13.3 and 12.6, which is 4.4 TB/s).
+constexpr int kStreamWaves = 12;
 
-template <int DT, int KC, int MT>
-__global__ __launch_bounds__(64 * kStreamWaves, 2) void i8_stream(PointArgs p, int groups) {
+template <int DT, int KC>
+__global__ __launch_bounds__(64 * kStreamWaves, 3) void i8_stream(PointArgs p, int groups) {
     extern __shared__ __align__(16) char lds[];                   // [groups][KC][4] fragments of 1 KB, then scales and biases
     lds_byte *const ldsb = (lds_byte *)lds;
     const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long rows = active_rows(p.count, p.cap, p.pixels);
-    long long row0 = ((long long)wave * gridDim.x + blockIdx.x) * (16 * MT);      // (few steps go to as many workgroups)
-    const long long stride = (long long)gridDim.x * kStreamWaves * (16 * MT);
-    if ((long long)blockIdx.x * (16 * MT) >= rows) return;
-    uint32_t arel[MT], k[KC];
+    long long row0 = ((long long)wave * gridDim.x + blockIdx.x) * 16;            // (few steps go to as many workgroups)
+    const long long stride = (long long)gridDim.x * kStreamWaves * 16;
+    if ((long long)blockIdx.x * 16 >= rows) return;
+    uint32_t k[KC];
 #pragma unroll
-    for (int i = 0; i < KC; ++i) k[i] = (uint32_t)(i * 64 + q * 16) < (uint32_t)p.pitch ? (uint32_t)(i * 64 + q * 16) : kOutOfRange;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) arel[m] = (uint32_t)(m * 16 + l16) * p.pitch;
+    for (int i = 0; i < KC; ++i) k[i] = (uint32_t)(i * 64 + q * 16) < (uint32_t)p.pitch ? (uint32_t)(l16 * p.pitch + i * 64 + q * 16) : kOutOfRange;
     struct Rows {
-        uint4 a[MT][KC];
-        float scale[MT];
+        uint4 a[KC];
+        float scale;
     };
     auto load = [&](Rows &o, long long at) __attribute__((always_inline)) {
-        const uint32_t here = (uint32_t)max(0LL, min(16LL * MT, rows - at));
+        const uint32_t here = (uint32_t)max(0LL, min(16LL, rows - at));
         const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a + (size_t)at * p.pitch), 0, (int)(here * p.pitch), kBufWord3);
         const __amdgpu_buffer_rsrc_t sr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a_scales + at), 0, (int)(here * 4), kBufWord3);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-#pragma unroll
-            for (int i = 0; i < KC; ++i) o.a[m][i] = buf_load16(ar, arel[m] + k[i]);       // (out of range plus a row's offset stays out of range)
-            o.scale[m] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sr, (m * 16 + l16) * 4, 0, 0));
-        }
+        for (int i = 0; i < KC; ++i) o.a[i] = buf_load16(ar, k[i]);
+        o.scale = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sr, l16 * 4, 0, 0));
     };
     const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc((void *)p.w, 0, (int)((uint32_t)p.N * p.pitch), kBufWord3);
     for (int f = wave; f < groups * KC * 4; f += kStreamWaves) {
@@ -440,36 +436,26 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void i8_stream(PointArgs p, i
     load(o0, row0);
     __syncthreads();
     auto step = [&](const Rows &o, long long at) __attribute__((always_inline)) {
+        const long long row = at + l16;
         for (int g = 0; g < groups; ++g) {
             const lds_byte *wf = ldsb + g * KC * 4096 + lane * 16;
-            i32x4 acc[MT][4];
+            i32x4 acc[4];
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int n = 0; n < 4; ++n) acc[m][n] = (i32x4){0, 0, 0, 0};
+            for (int n = 0; n < 4; ++n) acc[n] = (i32x4){0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < KC; ++i)
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const uint4 w = read16(wf + (i * 4 + n) * 1024);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) acc[m][n] = mfma_i8_16(w, o.a[m][i], acc[m][n]);
-                }
+                for (int n = 0; n < 4; ++n) acc[n] = mfma_i8_16(read16(wf + (i * 4 + n) * 1024), o.a[i], acc[n]);
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const int c = g * 64 + s * 32 + q * 8;
                 if (c >= p.N) continue;
-                float ws[8], bs[8];
+                float ws[8], bs[8], v[8];
                 load8(ws, sc + c);
                 load8(bs, sc + groups * 64 + c);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const long long row = at + m * 16 + l16;
-                    float v[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = finish(acc[m][2 * s + (e >> 2)][e & 3], o.scale[m], ws[e], bs[e], p.least);
-                    if (row < rows) store8<DT>(p.out, (size_t)row * p.N + c, v, p.N - c, p.wide && c + 8 <= p.N);
-                }
+                for (int e = 0; e < 8; ++e) v[e] = finish(acc[2 * s + (e >> 2)][e & 3], o.scale, ws[e], bs[e], p.least);
+                if (row < rows) store8<DT>(p.out, (size_t)row * p.N + c, v, p.N - c, p.wide && c + 8 <= p.N);
             }
         }
     };
@@ -507,12 +493,12 @@ size_t stream_lds(int KC, int N) {
     const size_t groups = (N + 63) / 64;
     return groups * (KC * 4096 + 512);
 }
-template <int DT, int KC, int MT>
+template <int DT, int KC>
 sbnet_status stream_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
-    const long long steps = (rows + 16 * MT - 1) / (16 * MT);
+    const long long steps = (rows + 15) / 16;
     const size_t lds = stream_lds(KC, p.N);
-    (void)hipFuncSetAttribute((const void *)i8_stream<DT, KC, MT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    hipLaunchKernelGGL((i8_stream<DT, KC, MT>), dim3((unsigned)(steps < 256 ? steps : 256)), dim3(64 * kStreamWaves), lds, s, p, (p.N + 63) / 64);
+    (void)hipFuncSetAttribute((const void *)i8_stream<DT, KC>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    hipLaunchKernelGGL((i8_stream<DT, KC>), dim3((unsigned)(steps < 256 ? steps : 256)), dim3(64 * kStreamWaves), lds, s, p, (p.N + 63) / 64);
     return launch_status(who);
 }
 
@@ -543,23 +529,26 @@ int cheapest(long long rows, int N, int pitch) {
     return best;
 }
 
-// Long lists whose weights fit LDS are streamed.  (us, streamed and the best of the others: 112640 x 256 x 64 11.4 and 12.5, 112640 x 64 x 256 14.4
-// and 21.8, 112640 x 256 x 256 21.8 and 24.2, 32768 x 64 x 256 8.2 and 9.8, 8192 x 256 x 64 4.9 and 4.9; but 8192 x 64 x 256 6.2 and 5.4, 32768 x
-// 256 x 256 11.6 and 10.6.)
+// Lists whose weights fit LDS are streamed from a length on that grows with them: every workgroup loads all.  (us, streamed and the best of the others,
+// below the line and above it: 64 -> 64, 4000 rows 4.0 and 4.0, 12000 4.1 and 4.6; 256 -> 128, 8192 5.6 and 4.9, 20000 6.4 and 6.7; 64 -> 256, 6000
+// 5.4 and 5.2, 20000 6.7 and 9.4; 256 -> 256, 16000 8.5 and 7.3, 30000 10.2 and 13.1; 64 -> 1024, 8192 12.9 and 9.7, 30000 15.3 and 24.9.  From 385 input
+// channels on the rows in flight are fewer: 512 -> 64, 20000 6.8 and 7.2, 512 -> 128, 50000 13.8 and 13.0.)
 bool streams(long long rows, int N, int KC) {
-    return KC <= 8 && stream_lds(KC <= 4 ? KC : KC <= 6 ? 6 : 8, N) <= 160 * 1024 && rows >= (N <= 64 ? 8192 : KC * N <= 512 ? 24576 : 65536);
+    if (KC > 8 || stream_lds(KC <= 4 ? KC : KC <= 6 ? 6 : 8, N) > 160 * 1024) return false;
+    const long long weights = (long long)KC * N;
+    return rows >= (KC <= 6 ? 4000 + 14 * weights : 60 * weights);
 }
 
 template <int DT>
 sbnet_status pointwise_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
     const int KC = (p.pitch + 63) / 64;
     if (streams(rows, p.N, KC)) {
-        if (KC == 1) return stream_go<DT, 1, 2>(who, p, rows, s);
-        if (KC == 2) return stream_go<DT, 2, 2>(who, p, rows, s);
-        if (KC == 3) return stream_go<DT, 3, 2>(who, p, rows, s);
-        if (KC == 4) return stream_go<DT, 4, 2>(who, p, rows, s);
-        if (KC <= 6) return stream_go<DT, 6, 2>(who, p, rows, s);
-        return stream_go<DT, 8, 2>(who, p, rows, s);
+        if (KC == 1) return stream_go<DT, 1>(who, p, rows, s);
+        if (KC == 2) return stream_go<DT, 2>(who, p, rows, s);
+        if (KC == 3) return stream_go<DT, 3>(who, p, rows, s);
+        if (KC == 4) return stream_go<DT, 4>(who, p, rows, s);
+        if (KC <= 6) return stream_go<DT, 6>(who, p, rows, s);
+        return stream_go<DT, 8>(who, p, rows, s);
     }
     switch (cheapest(rows, p.N, p.pitch)) {
         case 0: return direct_go<DT, 1, 1, 8>(who, p, rows, s);
