@@ -10,20 +10,36 @@ namespace {
 
 constexpr int kMaxPitch = 131056;
 
+// 32 output channels per workgroup.  Their weights are read twice, 32 neighbouring ones of an input channel at a time, for the largest and for the codes,
+// which change rows and columns in LDS: 128 input channels are 128 bytes of an output channel's row.
 template <int DT>
-__global__ __launch_bounds__(256) void i8_quantize_weights(const typename Elem<DT>::T *__restrict__ w, int Cin, int Cout, int pitch,
-                                                           int8_t *__restrict__ codes, float *__restrict__ scales) {
-    __shared__ uint32_t tops[256];
-    const int o = blockIdx.x;
+__global__ __launch_bounds__(1024) void i8_quantize_weights(const typename Elem<DT>::T *__restrict__ w, int Cin, int Cout, int pitch,
+                                                            int8_t *__restrict__ codes, float *__restrict__ scales) {
+    __shared__ uint32_t tile[32][33];
+    const int ch = threadIdx.x & 31, r = threadIdx.x >> 5;
+    const long long o = (long long)blockIdx.x * 32 + ch;
     uint32_t top = 0;
-    for (int c = threadIdx.x; c < Cin; c += 256) top = max(top, __float_as_uint(Elem<DT>::load(w + (size_t)c * Cout + o)) & 0x7fffffffu);
-    tops[threadIdx.x] = top;
+    if (o < Cout)
+        for (int c = r; c < Cin; c += 32) top = max(top, __float_as_uint(Elem<DT>::load(w + (size_t)c * Cout + o)) & 0x7fffffffu);
+    tile[r][ch] = top;
     __syncthreads();
-    for (int k = 0; k < 256; ++k) top = max(top, tops[k]);
+    for (int k = 0; k < 32; ++k) top = max(top, tile[k][ch]);
     const RowCode rc = row_code(top);
-    for (int c = threadIdx.x; c < pitch; c += 256)
-        codes[(size_t)o * pitch + c] = c < Cin ? code1(Elem<DT>::load(w + (size_t)c * Cout + o), rc.inv, code_keep(top)) : (int8_t)0;
-    if (threadIdx.x == 0) scales[o] = rc.scale;
+    const uint32_t keep = code_keep(top);
+    if (r == 0 && o < Cout) scales[o] = rc.scale;
+    const long long oo = (long long)blockIdx.x * 32 + r;          // the channel this thread writes
+    for (int c0 = 0; c0 < pitch; c0 += 128) {
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int c = c0 + 4 * r + k;
+            v[k] = o < Cout && c < Cin ? Elem<DT>::load(w + (size_t)c * Cout + o) : 0.f;
+        }
+        __syncthreads();
+        tile[ch][r] = codes4(v, rc.inv, keep);
+        __syncthreads();
+        if (oo < Cout && c0 + 4 * ch < pitch) *(uint32_t *)(codes + (size_t)oo * pitch + c0 + 4 * ch) = tile[r][ch];
+    }
 }
 
 struct PointArgs {
@@ -581,7 +597,7 @@ extern "C" sbnet_status sbnet_quantize_weights_i8(const void *w_hwio, sbnet_dtyp
     if (ranges_overlap(w_hwio, wb, w_codes, cb) || ranges_overlap(w_hwio, wb, w_scales, sb) || ranges_overlap(w_codes, cb, w_scales, sb))
         return fail(SBNET_EINVAL, "%s: arrays overlap", who);
     hipStream_t s = (hipStream_t)stream;
-#define SBNET_QW(DT) hipLaunchKernelGGL(i8_quantize_weights<DT>, dim3(Cout), dim3(256), 0, s, (const Elem<DT>::T *)w_hwio, Cin, Cout, \
+#define SBNET_QW(DT) hipLaunchKernelGGL(i8_quantize_weights<DT>, dim3((Cout + 31LL) / 32), dim3(1024), 0, s, (const Elem<DT>::T *)w_hwio, Cin, Cout, \
                                         pitch, w_codes, w_scales)
     if (dtype == SBNET_F32) SBNET_QW(SBNET_F32);
     else if (dtype == SBNET_BF16) SBNET_QW(SBNET_BF16);
