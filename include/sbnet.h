@@ -473,9 +473,9 @@ sbnet_status sbnet_conv_on_tiles_f8(const void *tiles_in_f8, const int32_t *coun
  * The norm is that of the rounded s, so that the two calls x + residual and norm give the same bits, and the gradient
  * below needs s alone.  Later tiles of y and sum are not touched.
  * x, residual, sum, y: [cap][pixels][C] in `dtype` (F32, BF16 or F16); residual and sum are both given or both NULL;
- * gain: device float32 [C] or NULL (1); eps positive and finite.  C at most 32768; pointers need their element's
+ * gain: device float32 [C] or NULL (1); eps a normal float32 number above 0.  C at most 32768; pointers need their element's
  * alignment only, 16 bytes with C * element size a multiple of 16 is fastest.  sum may be x or residual, y may be x or
- * residual, not both the same; other overlaps are refused.  A row whose squares pass float32's range gives zeros, one
+ * residual, not both the same; other overlaps of what is written are refused.  A row whose squares pass float32's range gives zeros, one
  * with an infinity or NaN gives NaN where it stands.
  *
  * sbnet_rms_norm_i8_on_tiles: the same s, and y in 8 bits, as sbnet_quantize_i8_on_tiles makes them of the unrounded
@@ -505,7 +505,7 @@ sbnet_status sbnet_quantize_i8_on_tiles(const void *x, sbnet_dtype dtype, const 
  * fp32 sums and arithmetic, dx rounded once to `dtype`; dgain's sums in a fixed order, no atomics: the same bits every
  * run for a given cap.  s, dy, dsum, dx: [cap][pixels][C]; later tiles of dx are not touched; dx may be s, dy or dsum (the
  * whole stack; other overlaps are refused).  workspace: device, 4-byte aligned, sbnet_rms_norm_backward_workspace_bytes(cap, pixels, C)
- * bytes, overwritten.
+ * bytes, overwritten; calls (or replays of captured ones) that may overlap in time need workspaces of their own.
  */
 size_t sbnet_rms_norm_backward_workspace_bytes(int cap, int pixels, int C);
 sbnet_status sbnet_rms_norm_backward_on_tiles(const void *s, const void *dy, const void *dsum, sbnet_dtype dtype,
@@ -517,8 +517,9 @@ sbnet_status sbnet_rms_norm_backward_on_tiles(const void *s, const void *dy, con
  * Pointwise (1x1, stride 1) convolution on tiles in 8-bit integers, with a scale for each pixel and each output channel:
  *   out[b][p][o] = act(sum over c of codes[b][p][c] * w_codes[o][c] * (scales[b][p] * w_scales[o]) + bias[o]),
  * act = ReLU when relu != 0, on the tiles b < min(*count, cap); later tiles are not touched.  The sum is exact (32-bit
- * integers); it is then converted to fp32, multiplied by scales[b][p], then by w_scales[o], the bias added (each rounded
- * to fp32), and the result rounded once to `dtype` (F32, BF16 or F16).  A NaN stays one through the ReLU.
+ * integers); it is then converted to fp32 and multiplied by scales[b][p], each rounded to fp32; the product by w_scales[o] and
+ * the bias are one fused step, and the result is rounded once to `dtype` (F32, BF16 or F16).  A NaN (a row's scale, say)
+ * stays one through the ReLU.
  * codes: int8 [cap][pixels][pitch] and scales: float32 [cap][pixels] as the two calls above write them; w_codes: int8
  * [Cout][pitch], w_scales: float32 [Cout]; bias: float32 [Cout] or NULL; out: [cap][pixels][Cout].  pitch: the input channels
  * rounded up to a multiple of 16 (the codes behind the last channel 0 on at least one side), at most 131056.  codes, w_codes and

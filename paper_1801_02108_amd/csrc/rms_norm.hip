@@ -294,7 +294,8 @@ sbnet_status check_rows(const char *who, sbnet_dtype dtype, int cap, int pixels,
 // two stacks of the same size either are the same or share nothing
 bool clash(const void *a, const void *b, size_t bytes) { return a && b && a != b && ranges_overlap(a, bytes, b, bytes); }
 
-bool eps_ok(float eps) { return eps > 0.f && eps * 0.f == 0.f; }
+// (of a row of zeros the reciprocal root is eps's alone)
+bool eps_ok(float eps) { return eps >= 1.17549435e-38f && eps * 0.f == 0.f; }
 
 template <class V>
 void rows_as(Form form, const RowArgs &p, size_t rows, hipStream_t s) {
@@ -333,7 +334,7 @@ sbnet_status rows_launch(const char *who, Form form, const void *x, const void *
     const sbnet_status st = check_rows(who, dtype, cap, pixels, C, kMaxC);
     if (st != SBNET_OK) return st;
     if (cap != 0 && !residual != !sum) return fail(SBNET_EINVAL, "%s: residual and sum are given together", who);
-    if (form != kCodes && !eps_ok(eps)) return fail(SBNET_EINVAL, "%s: eps must be positive and finite", who);
+    if (form != kCodes && !eps_ok(eps)) return fail(SBNET_EINVAL, "%s: eps must be a normal number above 0", who);
     const int es = elem_bytes(dtype), pitch = (C + 15) / 16 * 16;
     const uintptr_t stacks = (uintptr_t)x | (uintptr_t)residual | (uintptr_t)sum | (uintptr_t)y;
     if (stacks % es || ((uintptr_t)gain | (uintptr_t)scales | (uintptr_t)count) % 4)
@@ -342,7 +343,11 @@ sbnet_status rows_launch(const char *who, Form form, const void *x, const void *
     if ((y && y == sum) || clash(y, sum, bytes) || clash(y, x, bytes) || clash(y, residual, bytes) || clash(sum, x, bytes) ||
         clash(sum, residual, bytes))
         return fail(SBNET_EINVAL, "%s: stacks overlap", who);
+    for (const void *q : {(const void *)sum, (const void *)y})
+        if (q && gain && ranges_overlap(q, bytes, gain, (size_t)C * 4)) return fail(SBNET_EINVAL, "%s: a stack overlaps gain", who);
     if (codes) {
+        if (gain && (ranges_overlap(codes, rows * pitch, gain, (size_t)C * 4) || ranges_overlap(scales, rows * 4, gain, (size_t)C * 4)))
+            return fail(SBNET_EINVAL, "%s: a stack overlaps gain", who);
         const void *in[3] = {x, residual, sum};
         for (const void *q : in)
             if (q && (ranges_overlap(codes, rows * pitch, q, bytes) || ranges_overlap(scales, rows * 4, q, bytes)))
@@ -400,7 +405,7 @@ extern "C" sbnet_status sbnet_rms_norm_backward_on_tiles(const void *s, const vo
     if (!count || !dgain || !workspace || (cap != 0 && (!s || !dy || !dx))) return fail(SBNET_EINVAL, "%s: null pointer", who);
     const sbnet_status st = check_rows(who, dtype, cap, pixels, C, kMaxC);
     if (st != SBNET_OK) return st;
-    if (!eps_ok(eps)) return fail(SBNET_EINVAL, "%s: eps must be positive and finite", who);
+    if (!eps_ok(eps)) return fail(SBNET_EINVAL, "%s: eps must be a normal number above 0", who);
     const int es = elem_bytes(dtype);
     const uintptr_t stacks = (uintptr_t)s | (uintptr_t)dy | (uintptr_t)dsum | (uintptr_t)dx;
     if (stacks % es || ((uintptr_t)gain | (uintptr_t)dgain | (uintptr_t)count | (uintptr_t)workspace) % 4)
@@ -412,7 +417,10 @@ extern "C" sbnet_status sbnet_rms_norm_backward_on_tiles(const void *s, const vo
     for (const void *q : in)
         if (q && (ranges_overlap(dgain, (size_t)C * 4, q, bytes) || ranges_overlap(workspace, need, q, bytes)))
             return fail(SBNET_EINVAL, "%s: stacks overlap", who);
-    if (ranges_overlap(dgain, (size_t)C * 4, workspace, need)) return fail(SBNET_EINVAL, "%s: workspace overlaps dgain", who);
+    const size_t cb = (size_t)C * 4;
+    if (gain && (ranges_overlap(dx, bytes, gain, cb) || ranges_overlap(dgain, cb, gain, cb) || ranges_overlap(workspace, need, gain, cb)))
+        return fail(SBNET_EINVAL, "%s: a result or the workspace overlaps gain", who);
+    if (ranges_overlap(dgain, cb, workspace, need)) return fail(SBNET_EINVAL, "%s: workspace overlaps dgain", who);
     BackArgs p = {};
     p.s = s; p.dy = dy; p.dsum = dsum; p.dx = dx; p.gain = gain; p.count = count;
     p.eps = eps; p.inv_c = 1.f / (float)C; p.cap = cap; p.pixels = pixels; p.C = C;

@@ -284,6 +284,18 @@ def test_rows_of_zeros_infinities_nans_and_extremes(C, dtype):
     assert torch.equal(out.isnan().all(-1), scales.isnan()) and torch.equal(out.isnan().any(-1), scales.isnan())
 
 
+@pytest.mark.parametrize("eps", [1.1754944e-38, 1e-30, 1e30])
+def test_the_ends_of_eps(eps):
+    step("eps %g" % eps)
+    x = stack(rnd(52), 2, 3, 40, "f32")
+    x[0] = 0
+    y, _ = sb.rms_norm_on_tiles(x, cnt(2), eps=eps)
+    close_norm(host(y), host(x), None, "f32", "norm", eps)
+    dx, dgain = sb.rms_norm_backward_on_tiles(x, torch.ones_like(x), cnt(2), eps=eps)
+    with np.errstate(over="ignore", invalid="ignore"):
+        check_gradients(x, torch.ones_like(x), None, None, 2, dx, dgain, "f32", float(np.float32(eps)))
+
+
 # ---- weights and product -------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("cin,cout", [(1, 1), (3, 5), (16, 8), (64, 256), (100, 33), (256, 64), (777, 130), (4100, 70), (64, 1025)])
