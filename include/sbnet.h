@@ -482,8 +482,8 @@ sbnet_status sbnet_conv_on_tiles_f8(const void *tiles_in_f8, const int32_t *coun
  * (fp32) y.  codes: int8 [cap][pixels][pitch], scales: float32 [cap][pixels].
  *
  * sbnet_quantize_i8_on_tiles: one scale for each row v (a pixel's channels),
- *   t = max(2^-100, max over c of |v[c]|),  scale = t / 127,  codes[c] = round(v[c] * (127 / t)) to nearest even, in fp32
- * (both quotients rounded to fp32), so that v[c] is about codes[c] * scale; codes are in -127 .. 127.  pitch is C rounded up
+ *   t = max(2^-100, max over c of |v[c]|),  scale = t / 127,  codes[c] = round(v[c] * (127 * (1 / t))) to nearest even, in
+ * fp32 (every quotient and product rounded), so that v[c] is about codes[c] * scale; codes are in -127 .. 127.  pitch is C rounded up
  * to a multiple of 16, and the codes behind C are written as 0.  A row that holds an infinity or NaN gets scale NaN and
  * codes 0.
  */

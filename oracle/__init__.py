@@ -346,13 +346,13 @@ def rms_norm_backward(s, dy, gain=None, dsum=None, eps=1e-6):
 
 def quantize_i8(v):
     """(codes, scales) of the rows of v, in float32 as the quantiser is defined: t = max(2^-100, max |v|), scale = t / 127,
-    code = nearest even whole number to v * (127 / t); rows with an infinity or NaN: scale NaN, codes 0.  Rows of codes
+    code = nearest even whole number to v * (127 * (1 / t)); rows with an infinity or NaN: scale NaN, codes 0.  Rows of codes
     are padded with zeros to a multiple of 16."""
     v = np.asarray(v, dtype=np.float32)
     fine = np.isfinite(v).all(-1)
     v = np.where(fine[..., None], v, np.float32(0))
     t = np.maximum(np.abs(v).max(-1), np.float32(2.0) ** -100)
-    codes = np.rint(v * (np.float32(127) / t)[..., None]).astype(np.int8)
+    codes = np.rint(v * (np.float32(127) * (np.float32(1) / t))[..., None]).astype(np.int8)
     pad = [(0, 0)] * (v.ndim - 1) + [(0, -v.shape[-1] % 16)]
     return np.pad(codes, pad), np.where(fine, t / np.float32(127), np.float32(np.nan))
 

@@ -14,7 +14,7 @@ constexpr float kLeastTop = 7.888609052210118e-31f;                  // 2^-100
 constexpr uint32_t kInfBits = 0x7f800000u;
 
 // The 8-bit form of a row whose largest magnitude has the bits `top` (as an unsigned number: NaN is above infinity, infinity
-// above everything finite).  Below 2^-100 the scale stays where it is: 127 / t must not overflow.
+// above everything finite).  Below 2^-100 the scale stays where it is: the reciprocal must not overflow.
 struct RowCode {
     float inv, scale;
 };
@@ -26,11 +26,11 @@ __device__ __forceinline__ RowCode row_code(uint32_t top) {
         return r;
     }
     const float t = fmaxf(__uint_as_float(top), kLeastTop);
-    r.inv = 127.f / t;
+    r.inv = 127.f * (1.f / t);
     r.scale = t / 127.f;
     return r;
 }
-// Four codes as bytes.  |v * inv| <= 127 (1 + 2^-23) is first rounded to fp32; added to 3 * 2^22 it is rounded to the nearest whole number,
+// Four codes as bytes.  |v * inv| <= 127 (1 + 2^-21) is first rounded to fp32; added to 3 * 2^22 it is rounded to the nearest whole number,
 // ties to even, whose lowest byte is that of the sum's bits.  `keep` is 0 for a row that is not finite, else all ones.
 __device__ __forceinline__ uint32_t codes4(const float *v, float inv, uint32_t keep) {
 #pragma clang fp contract(off)
