@@ -2,7 +2,7 @@
 // bias[o]), acc = sum over the channels of code * weight code, exact in 32 bits (131056 products of at most 2^14).
 //
 //   i8_quantize_weights  [1][1][Cin][Cout] -> [Cout][pitch] codes and a scale for each output channel
-//   i8_tiles, i8_direct  the product
+//   i8_tiles, i8_direct, i8_stream  the product: large, of few rows, of long lists with few weights
 #include "rows.h"
 
 namespace sbnet {
@@ -109,6 +109,9 @@ constexpr int kStageK = 128;                      // bytes of a row in a stage
 
 // Waves 0 .. 3 multiply, WM x WN of them, each MF x NF blocks of 32 x 32; waves 4 .. 7 move the operands from memory to LDS, up to two stages ahead,
 // across the borders of tiles.  One barrier a stage: before it stage k has been read to the end and stage k + 1 has landed.
+// Bound, one workgroup a CU, by the CU's intake (a stage takes about 15 ns a KB: 0.70 us for 256 x 128, whose matrix steps are 0.43), and on the whole card by its
+// power (the clock falls to 1.76 GHz).  8192 x 4096 x 8192: 263 us, 2.1 POP/s; 4096 x 4096 x 4096 65 us.  Moving waves of their own because a wave stands at
+// the copies that it asks for: 329 us where the multiplying waves ask.
 template <int DT, int WM, int WN, int MF, int NF>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void i8_tiles(PointArgs p) {
@@ -287,7 +290,8 @@ float as[MF];
 // ---- small products: 16 MT rows x 16 NT channels per workgroup, operands from memory to registers, the channels summed over split between its waves
 // 16 x 16 x 64 steps, weights as the first operand again.  Wave w of KS takes the pieces of 128 bytes w, w + KS, ... of every row; the waves' sums
 // meet in LDS.  Frag n of NT holds channels 4 NT q + 4 n + r in its row 4 q + r, which gives a lane 4 NT neighbouring channels.
-// Bound by latency (few rows: by the weights' bytes): every wave has U pieces of all its rows in flight, twice.
+// Bound by latency (few rows: by the weights' bytes): every wave has U pieces of all its rows in flight, twice.  1 x 4096 x 4096: 5.4 us, 2.7 of them
+// the launch, 6 TB/s for the rest; 23 x 2056 x 5125 5.8 us; 300 x 368 x 360 4.1 us.
 __device__ __forceinline__ i32x4 mfma_i8_16(uint4 a, uint4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }
