@@ -414,7 +414,18 @@ __global__ __launch_bounds__(64 * KS) void i8_direct(PointArgs p) {
 // a wave is 64 bytes of each of 16 rows.
 // Bound by memory: the next 16 rows are requested before these are multiplied, by twelve waves a CU (eight waves of 32 rows: 112640 x 256 x 256
 // 22.0 us instead of 20.2, 142560 x 256 x 64 13.3 and 12.6, which is 4.4 TB/s).
+//
+// Results no wider than the input (in channels) are written past the cache, which is left to the codes, in whole lines: 112640 x 128 x 128 11.9 us and, with a
+// pass over the results behind it, 21.5; so 8.9 and 21.0; 142560 x 256 x 64 13.1 and 20.0, 12.0 and 20.0; 112640 x 256 x 256 21.4 and 40.0, 18.7 and 39.3.
+// Wider ones gain alone and lose with who reads them: 60000 x 64 x 512 15.8 and 34.0, 14.4 and 35.5.
 constexpr int kStreamWaves = 12;
+
+// lanes 8 .. 15 of each 16 of a with lanes 0 .. 7 of b
+__device__ __forceinline__ void swap8(uint32_t &a, uint32_t &b) {
+    const uint32_t u = (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)b, 0x128, 0xf, 0xc, false);      // row_ror:8 into the upper eight
+    b = (uint32_t)__builtin_amdgcn_update_dpp((int)b, (int)a, 0x128, 0xf, 0x3, false);
+    a = u;
+}
 
 template <int DT, int KC>
 __global__ __launch_bounds__(64 * kStreamWaves, 3) void i8_stream(PointArgs p, int groups) {
@@ -452,6 +463,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 3) void i8_stream(PointArgs p, i
         sc[c] = c < p.N ? p.w_scales[c] : 0.f;
         sc[groups * 64 + c] = c < p.N && p.bias ? p.bias[c] : 0.f;
     }
+    const bool past_cache = DT != SBNET_F32 && p.wide && p.N <= p.pitch;
     Rows o0, o1;
     load(o0, row0);
     __syncthreads();
@@ -466,16 +478,33 @@ __global__ __launch_bounds__(64 * kStreamWaves, 3) void i8_stream(PointArgs p, i
             for (int i = 0; i < KC; ++i)
 #pragma unroll
                 for (int n = 0; n < 4; ++n) acc[n] = mfma_i8_16(read16(wf + (i * 4 + n) * 1024), o.a[i], acc[n]);
+            float v[2][8];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float ws[8], bs[8];
+                load8(ws, sc + g * 64 + s * 32 + q * 8);
+                load8(bs, sc + (groups + g) * 64 + s * 32 + q * 8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[s][e] = finish(acc[2 * s + (e >> 2)][e & 3], o.scale, ws[e], bs[e], p.least);
+            }
+            if (past_cache && g * 64 + 64 <= p.N) {               // 128 bytes of each of 8 rows a store
+                u32x4 a, b;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    uint32_t u = pack2<DT>(v[0][2 * w], v[0][2 * w + 1]), t = pack2<DT>(v[1][2 * w], v[1][2 * w + 1]);
+                    swap8(u, t);
+                    a[w] = u;
+                    b[w] = t;
+                }
+                uint16_t *to = (uint16_t *)p.out + (size_t)(at + (l16 & 7)) * p.N + g * 64 + (l16 >> 3) * 32 + q * 8;
+                if (at + (l16 & 7) < rows) __builtin_nontemporal_store(a, (u32x4 *)to);
+                if (at + 8 + (l16 & 7) < rows) __builtin_nontemporal_store(b, (u32x4 *)(to + (size_t)8 * p.N));
+                continue;
+            }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const int c = g * 64 + s * 32 + q * 8;
-                if (c >= p.N) continue;
-                float ws[8], bs[8], v[8];
-                load8(ws, sc + c);
-                load8(bs, sc + groups * 64 + c);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = finish(acc[2 * s + (e >> 2)][e & 3], o.scale, ws[e], bs[e], p.least);
-                if (row < rows) store8<DT>(p.out, (size_t)row * p.N + c, v, p.N - c, p.wide && c + 8 <= p.N);
+                if (c < p.N && row < rows) store8<DT>(p.out, (size_t)row * p.N + c, v[s], p.N - c, p.wide && c + 8 <= p.N);
             }
         }
     };

@@ -131,9 +131,10 @@ struct Piece {
         const uint4 q = buf_load16(s.r, Span<DT>::place(i, left));
         w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
     }
-    __device__ __forceinline__ void store(const Span<DT> &s, uint32_t i, int left) const {
+    __device__ __forceinline__ void store(const Span<DT> &s, uint32_t i, int left, bool past_cache = false) const {
         const u32x4 v = {w[0], w[1], w[2], w[3]};
-        __builtin_amdgcn_raw_buffer_store_b128(v, s.r, (int)Span<DT>::place(i, left), 0, 0);
+        if (past_cache) __builtin_amdgcn_raw_buffer_store_b128(v, s.r, (int)Span<DT>::place(i, left), 0, 2);      // non-temporal
+        else __builtin_amdgcn_raw_buffer_store_b128(v, s.r, (int)Span<DT>::place(i, left), 0, 0);
     }
     __device__ __forceinline__ float get(int e) const {
         if (DT == SBNET_F32) return __uint_as_float(w[e]);
@@ -155,7 +156,7 @@ struct Single {
         const int at = (int)Span<DT>::place(i, left);
         w = DT == SBNET_F32 ? __builtin_amdgcn_raw_buffer_load_b32(s.r, at, 0, 0) : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(s.r, at, 0, 0);
     }
-    __device__ __forceinline__ void store(const Span<DT> &s, uint32_t i, int left) const {
+    __device__ __forceinline__ void store(const Span<DT> &s, uint32_t i, int left, bool = false) const {
         const int at = (int)Span<DT>::place(i, left);
         if (DT == SBNET_F32) __builtin_amdgcn_raw_buffer_store_b32(w, s.r, at, 0, 0);
         else __builtin_amdgcn_raw_buffer_store_b16((unsigned short)w, s.r, at, 0, 0);
