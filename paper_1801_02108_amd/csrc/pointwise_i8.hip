@@ -87,20 +87,35 @@ __device__ __forceinline__ void load8(float *v, const float *p) {
     }
 }
 
-// the results of 8 neighbouring channels of one row; `wide`: they all exist and 16-byte stores fit
+// The results of 8 (4) neighbouring channels of one row, `left` of them there are.  Where rows do not start at multiples of 16 bytes the memory units take
+// the same stores at any address: single ones take longer (33280 x 928 x 419 35 us, with eight single stores 69; 112640 x 64 x 250 17 and 64).
+typedef uint32_t any_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t any_u32x2 __attribute__((ext_vector_type(2), aligned(2)));
 template <int DT>
-__device__ __forceinline__ void store8(void *out, size_t at, const float *v, int left, bool wide) {
+__device__ __forceinline__ void store8(void *out, size_t at, const float *v, int left) {
     typedef typename Elem<DT>::T T;
-    if (wide) {
+    if (left >= 8) {
         if (DT == SBNET_F32) {
-            *(float4 *)((T *)out + at) = make_float4(v[0], v[1], v[2], v[3]);
-            *(float4 *)((T *)out + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            *(any_u32x4 *)((T *)out + at) = (any_u32x4){__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+            *(any_u32x4 *)((T *)out + at + 4) = (any_u32x4){__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
         } else {
-            *(uint4 *)((T *)out + at) = make_uint4(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]), pack2<DT>(v[4], v[5]), pack2<DT>(v[6], v[7]));
+            *(any_u32x4 *)((T *)out + at) = (any_u32x4){pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]), pack2<DT>(v[4], v[5]), pack2<DT>(v[6], v[7])};
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < 7; ++k)
+            if (k < left) Elem<DT>::store((T *)out + at + k, v[k]);
+    }
+}
+template <int DT>
+__device__ __forceinline__ void store4(void *out, size_t at, const float *v, int left) {
+    typedef typename Elem<DT>::T T;
+    if (left >= 4) {
+        if (DT == SBNET_F32) *(any_u32x4 *)((T *)out + at) = (any_u32x4){__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        else *(any_u32x2 *)((T *)out + at) = (any_u32x2){pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
+    } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
             if (k < left) Elem<DT>::store((T *)out + at + k, v[k]);
     }
 }
@@ -273,14 +288,13 @@ float as[MF];
                     float ws[8], bs[8];
                     load8(ws, sc + BM + c);
                     load8(bs, sc + BM + BN + c);
-                    const bool wide = p.wide && n0 + c + 8 <= p.N;
 #pragma unroll
                     for (int m = 0; m < MF; ++m) {
                         const long long row = row0 + (wm * MF + m) * 32 + l32;
                         float v[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[e] = finish(acc[m][n][8 * g + e], as[m], ws[e], bs[e], p.least);
-                        if (row < rows) store8<DT>(p.out, (size_t)row * p.N + n0 + c, v, p.N - n0 - c, wide);
+                        if (row < rows) store8<DT>(p.out, (size_t)row * p.N + n0 + c, v, p.N - n0 - c);
                     }
                 }
         }
@@ -294,19 +308,6 @@ float as[MF];
 // the launch, 6 TB/s for the rest; 23 x 2056 x 5125 5.8 us; 300 x 368 x 360 4.1 us.
 __device__ __forceinline__ i32x4 mfma_i8_16(uint4 a, uint4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
-}
-
-template <int DT>
-__device__ __forceinline__ void store4(void *out, size_t at, const float *v, int left, bool wide) {
-    typedef typename Elem<DT>::T T;
-    if (wide) {
-        if (DT == SBNET_F32) *(float4 *)((T *)out + at) = make_float4(v[0], v[1], v[2], v[3]);
-        else *(uint2 *)((T *)out + at) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (k < left) Elem<DT>::store((T *)out + at + k, v[k]);
-    }
 }
 
 template <int DT, int MT, int NT, int KS>
@@ -404,7 +405,7 @@ __global__ __launch_bounds__(64 * KS) void i8_direct(PointArgs p) {
         const int r = m * 16 + l16, c = n0 + 4 * NT * q + 4 * n;
         const float v[4] = {finish(t.x, as[i], ws[i][0], bs[i][0], p.least), finish(t.y, as[i], ws[i][1], bs[i][1], p.least),
                             finish(t.z, as[i], ws[i][2], bs[i][2], p.least), finish(t.w, as[i], ws[i][3], bs[i][3], p.least)};
-        if ((uint32_t)r < here) store4<DT>(p.out, (size_t)(row0 + r) * p.N + c, v, p.N - c, p.wide && c + 4 <= p.N);
+        if ((uint32_t)r < here) store4<DT>(p.out, (size_t)(row0 + r) * p.N + c, v, p.N - c);
     }
 }
 
@@ -504,7 +505,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 3) void i8_stream(PointArgs p, i
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const int c = g * 64 + s * 32 + q * 8;
-                if (c < p.N && row < rows) store8<DT>(p.out, (size_t)row * p.N + c, v[s], p.N - c, p.wide && c + 8 <= p.N);
+                if (c < p.N && row < rows) store8<DT>(p.out, (size_t)row * p.N + c, v[s], p.N - c);
             }
         }
     };
