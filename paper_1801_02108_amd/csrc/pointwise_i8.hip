@@ -125,7 +125,7 @@ constexpr int kStageK = 128;                      // bytes of a row in a stage
 // Waves 0 .. 3 multiply, WM x WN of them, each MF x NF blocks of 32 x 32; waves 4 .. 7 move the operands from memory to LDS, up to two stages ahead,
 // across the borders of tiles.  One barrier a stage: before it stage k has been read to the end and stage k + 1 has landed.
 // Bound, one workgroup a CU, by the CU's intake (a stage takes about 15 ns a KB: 0.70 us for 256 x 128, whose matrix steps are 0.43), and on the whole card by its
-// power (the clock falls to 1.76 GHz).  8192 x 4096 x 8192: 263 us, 2.1 POP/s; 4096 x 4096 x 4096 65 us.  Moving waves of their own because a wave stands at
+// power (the clock falls to 1.76 GHz).  8192 x 4096 x 8192: 248 to 265 us, 2.1 to 2.2 POP/s; 4096 x 4096 x 4096 65 us.  Moving waves of their own because a wave stands at
 // the copies that it asks for: 329 us where the multiplying waves ask.
 template <int DT, int WM, int WN, int MF, int NF>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))

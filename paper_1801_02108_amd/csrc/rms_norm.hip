@@ -5,9 +5,9 @@
 //   rms_backward_rows  with h = s r:  dx = r (gain dy - h mean(gain dy h)) + dsum,  partial sums of dgain = dy h
 //   rms_dgain_sum      adds the partial sums in a fixed order
 //
-// Bound by memory: a row is read once, stays in registers over its sums, and is written once.  112640 rows of 256 bf16: with the residual 44 us (5.2 TB/s; a
-// large copy reaches 5.0), in 8 bits from 44288 rows of 384 21 us (5.7 TB/s), without a norm from 142560 of 256 20.6 us (5.3 TB/s); gradients with the one past
-// the norm 41.8 us (5.5 TB/s) and 4 for the sums of dgain; 4099 rows of 4096 f32 22 us (6.0 TB/s).
+// Bound by memory: a row is read once, stays in registers over its sums, and is written once.  112640 rows of 256 bf16: with the residual 40 us (5.8 TB/s; a
+// large copy reaches 5.0), in 8 bits from 44288 rows of 384 21 to 24 us (5.0 to 5.7 TB/s), without a norm from 142560 of 256 18 to 21 us (5.3 to 6.2 TB/s);
+// gradients with the one past the norm 41 us (5.6 TB/s) and 4 for the sums of dgain; 4099 rows of 4096 f32 22 us (6.1 TB/s).
 #include "rows.h"
 
 namespace sbnet {
