@@ -190,7 +190,8 @@ void i8_tiles(PointArgs p) {
             if (ks == 0) {                        // the tile's scales and biases, 64 at a time
                 const __amdgpu_buffer_rsrc_t sr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a_scales + row0), 0, (int)(here * 4), kBufWord3);
                 const __amdgpu_buffer_rsrc_t cr = __builtin_amdgcn_make_buffer_rsrc((void *)(p.w_scales + n0), 0, (int)(wide * 4), kBufWord3);
-                const __amdgpu_buffer_rsrc_t br = __builtin_amdgcn_make_buffer_rsrc((void *)(p.bias ? p.bias + n0 : p.w_scales), 0, p.bias ? (int)(wide * 4) : 0, kBufWord3);
+                const __amdgpu_buffer_rsrc_t br = __builtin_amdgcn_make_buffer_rsrc((void *)(p.bias ? p.bias + n0 : p.w_scales), 0,
+                                                                                     p.bias ? (int)(wide * 4) : 0, kBufWord3);
                 lds_byte *st = scaleb + (j & 3) * kScales;
 #pragma unroll
                 for (int i = 0; i < kScaleEach; ++i) {
@@ -276,7 +277,7 @@ void i8_tiles(PointArgs p) {
             int n0;
             tile_at(j, row0, n0);
             const float *sc = (const float *)(lds + 3 * kStage + (j & 3) * kScales);
-float as[MF];
+            float as[MF];
 #pragma unroll
             for (int m = 0; m < MF; ++m) as[m] = sc[(wm * MF + m) * 32 + l32];
 #pragma unroll
@@ -457,7 +458,8 @@ __global__ __launch_bounds__(64 * kStreamWaves, 3) void i8_stream(PointArgs p, i
     for (int f = wave; f < groups * KC * 4; f += kStreamWaves) {
         const int g = f / (KC * 4), i = f / 4 % KC, n = f % 4;
         const uint32_t at = (uint32_t)(i * 64 + q * 16), o = (uint32_t)(g * 64 + (n >> 1) * 32 + (l16 >> 2) * 8 + (n & 1) * 4 + (l16 & 3));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(ldsb + f * 1024), 16, (int)(at < (uint32_t)p.pitch ? o * p.pitch + at : kOutOfRange), 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(ldsb + f * 1024), 16,
+                                                 (int)(at < (uint32_t)p.pitch ? o * p.pitch + at : kOutOfRange), 0, 0, 0);
     }
     float *const sc = (float *)(lds + groups * KC * 4096);       // [groups][64] scales, then biases
     for (int c = threadIdx.x; c < groups * 64; c += 64 * kStreamWaves) {

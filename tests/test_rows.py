@@ -63,7 +63,8 @@ REFUSED = [
     (norm, dict(res=C_, total=D, y=D), sb.EINVAL, "overlap"), (norm, dict(res=C_, total=off(C_, 128)), sb.EINVAL, "overlap"),
     (norm, dict(res=C_, total=off(D, 2)), sb.EINVAL, "overlap"), (norm, dict(gain=D), sb.EINVAL, "gain"), (norm, dict(eps=1e-39), sb.EINVAL, "eps"),
     (norm_i8, dict(gain=off(E, 64)), sb.EINVAL, "gain"), (norm_i8, dict(gain=D), sb.EINVAL, "gain"), (norm_i8, dict(res=C_, total=F_, gain=F_), sb.EINVAL, "gain"),
-    (backward, dict(gain=E), sb.EINVAL, "gain"), (backward, dict(gain=off(D, 8)), sb.EINVAL, "gain"), (backward, dict(gain=F_), sb.EINVAL, "gain"), (norm, dict(res=C_, total=E, y=off(C_, 4 * 9 * 64 * 2 - 2)), sb.EINVAL, "overlap"),
+    (backward, dict(gain=E), sb.EINVAL, "gain"), (backward, dict(gain=off(D, 8)), sb.EINVAL, "gain"), (backward, dict(gain=F_), sb.EINVAL, "gain"),
+    (norm, dict(res=C_, total=E, y=off(C_, 4 * 9 * 64 * 2 - 2)), sb.EINVAL, "overlap"),
     (norm_i8, dict(codes=None), sb.EINVAL, "null"), (norm_i8, dict(scales=None), sb.EINVAL, "null"),
     (norm_i8, dict(eps=0.0), sb.EINVAL, "eps"), (norm_i8, dict(codes=A), sb.EINVAL, "overlap"), (norm_i8, dict(scales=D), sb.EINVAL, "overlap"),
     (norm_i8, dict(res=C_, total=D), sb.EINVAL, "overlap"), (norm_i8, dict(scales=off(E, 1)), sb.EINVAL, "aligned"),
