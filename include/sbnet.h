@@ -484,7 +484,7 @@ sbnet_status sbnet_conv_on_tiles_f8(const void *tiles_in_f8, const int32_t *coun
  * sbnet_quantize_i8_on_tiles: one scale for each row v (a pixel's channels),
  *   t = max(2^-100, max over c of |v[c]|),  scale = t / 127,  codes[c] = round(v[c] * (127 * (1 / t))) to nearest even, in
  * fp32 (every quotient and product rounded), so that v[c] is about codes[c] * scale; codes are in -127 .. 127.  pitch is C rounded up
- * to a multiple of 16, and the codes behind C are written as 0.  A row that holds an infinity or NaN gets scale NaN and
+ * to a multiple of 16, and the codes behind C are written as 0; C at most 32768.  A row that holds an infinity or NaN gets scale NaN and
  * codes 0.
  */
 sbnet_status sbnet_rms_norm_on_tiles(const void *x, const void *residual, sbnet_dtype dtype, const int32_t *count,
@@ -502,7 +502,7 @@ sbnet_status sbnet_quantize_i8_on_tiles(const void *x, sbnet_dtype dtype, const 
  * the tiles b < min(*count, cap):
  *   dx = r * (gain * dy - h * mean over c of (gain * dy * h)) + dsum    (the gradient of x and of the residual),
  *   dgain[c] = sum over the rows of dy * h                              (device float32 [C], written; zeros without rows).
- * fp32 sums and arithmetic, dx rounded once to `dtype`; dgain's sums in a fixed order, no atomics: the same bits every
+ * fp32 sums and arithmetic, dx rounded once to `dtype`; C at most 32768; dgain's sums in a fixed order, no atomics: the same bits every
  * run for a given cap.  s, dy, dsum, dx: [cap][pixels][C]; later tiles of dx are not touched; dx may be s, dy or dsum (the
  * whole stack; other overlaps are refused).  workspace: device, 4-byte aligned, sbnet_rms_norm_backward_workspace_bytes(cap, pixels, C)
  * bytes, overwritten; calls (or replays of captured ones) that may overlap in time need workspaces of their own.
@@ -522,11 +522,11 @@ sbnet_status sbnet_rms_norm_backward_on_tiles(const void *s, const void *dy, con
  * stays one through the ReLU.
  * codes: int8 [cap][pixels][pitch] and scales: float32 [cap][pixels] as the two calls above write them; w_codes: int8
  * [Cout][pitch], w_scales: float32 [Cout]; bias: float32 [Cout] or NULL; out: [cap][pixels][Cout].  pitch: the input channels
- * rounded up to a multiple of 16 (the codes behind the last channel 0 on at least one side), at most 131056.  codes, w_codes and
- * out 16-byte aligned.
+ * rounded up to a multiple of 16 (the codes behind the last channel 0 on at least one side), at most 131056; Cout at most 2^26.
+ * codes, w_codes and out 16-byte aligned.
  *
  * sbnet_quantize_weights_i8: w_hwio [1][1][Cin][Cout] in `dtype` -> w_codes [Cout][pitch], w_scales [Cout], each output
- * channel's weights quantised as a row above.  Cin at most 131056.
+ * channel's weights quantised as a row above.  Cin at most 131056, Cout at most 2^26.
  */
 sbnet_status sbnet_quantize_weights_i8(const void *w_hwio, sbnet_dtype dtype, int Cin, int Cout, int8_t *w_codes,
                                        float *w_scales, void *stream);

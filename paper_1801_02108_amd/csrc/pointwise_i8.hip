@@ -8,7 +8,7 @@
 namespace sbnet {
 namespace {
 
-constexpr int kMaxPitch = 131056;
+constexpr int kMaxPitch = 131056, kMaxCout = 1 << 26;
 
 // 32 output channels per workgroup.  Their weights are read twice, 32 neighbouring ones of an input channel at a time, for the largest and for the codes,
 // which change rows and columns in LDS: 128 input channels are 128 bytes of an output channel's row.
@@ -536,7 +536,6 @@ sbnet_status tiles_go(const char *who, const PointArgs &p, long long rows, hipSt
 template <int DT, int MT, int NT, int KS>
 sbnet_status direct_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
     const long long tiles = (rows + 16 * MT - 1) / (16 * MT) * (((long long)p.N + 16 * NT - 1) / (16 * NT));
-    if (tiles >= 1LL << 30) return fail(SBNET_EUNSUPPORTED, "%s: too many output channels", who);
     hipLaunchKernelGGL((i8_direct<DT, MT, NT, KS>), dim3((unsigned)tiles), dim3(64 * KS), 0, s, p);
     return launch_status(who);
 }
@@ -626,6 +625,7 @@ extern "C" sbnet_status sbnet_quantize_weights_i8(const void *w_hwio, sbnet_dtyp
     if (!is_float_dtype(dtype)) return fail(SBNET_EUNSUPPORTED, "%s: dtype must be f32, bf16 or f16", who);
     if (Cin <= 0 || Cout <= 0) return fail(SBNET_EINVAL, "%s: bad sizes", who);
     if (Cin > kMaxPitch) return fail(SBNET_EUNSUPPORTED, "%s: more than %d input channels", who, kMaxPitch);
+    if (Cout > kMaxCout) return fail(SBNET_EUNSUPPORTED, "%s: more than %d output channels", who, kMaxCout);
     if ((uintptr_t)w_hwio % elem_bytes(dtype) || ((uintptr_t)w_scales & 3) || ((uintptr_t)w_codes & 15))
         return fail(SBNET_EINVAL, "%s: a pointer is not aligned (codes to 16 bytes, others to their elements)", who);
     const int pitch = (Cin + 15) / 16 * 16;
@@ -651,6 +651,7 @@ extern "C" sbnet_status sbnet_pointwise_i8_on_tiles(const int8_t *codes, const f
     if (cap < 0 || pixels <= 0 || pitch <= 0 || Cout <= 0) return fail(SBNET_EINVAL, "%s: bad sizes", who);
     if (pitch % 16) return fail(SBNET_EUNSUPPORTED, "%s: the pitch of the codes must be a multiple of 16", who);
     if (pitch > kMaxPitch) return fail(SBNET_EUNSUPPORTED, "%s: more than %d input channels", who, kMaxPitch);
+    if (Cout > kMaxCout) return fail(SBNET_EUNSUPPORTED, "%s: more than %d output channels", who, kMaxCout);
     if ((long long)cap * pixels >= (1LL << 31)) return fail(SBNET_EUNSUPPORTED, "%s: too many rows", who);
     if (((uintptr_t)codes | (uintptr_t)w_codes | (uintptr_t)out) & 15)
         return fail(SBNET_EINVAL, "%s: codes, w_codes and out must be 16-byte aligned", who);

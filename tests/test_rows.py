@@ -88,6 +88,7 @@ REFUSED = [
     (pointwise, dict(bias=off(F_, 1 << 20 | 2)), sb.EINVAL, "aligned"), (pointwise, dict(out=A), sb.EINVAL, "overlap"),
     (pointwise, dict(out=D), sb.EINVAL, "overlap"), (pointwise, dict(bias=F_), sb.EINVAL, "overlap"),
     (pointwise, dict(cap=1 << 16, pixels=1 << 15), sb.EUNSUPPORTED, "rows"),
+    (pointwise, dict(cout=(1 << 26) + 1), sb.EUNSUPPORTED, "output channels"), (weights, dict(cout=(1 << 31) - 1), sb.EUNSUPPORTED, "output channels"),
 ]
 
 
