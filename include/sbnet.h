@@ -476,7 +476,7 @@ sbnet_status sbnet_conv_on_tiles_f8(const void *tiles_in_f8, const int32_t *coun
  * gain: device float32 [C] or NULL (1); eps a normal float32 number above 0.  C at most 32768; pointers need their element's
  * alignment only, 16 bytes with C * element size a multiple of 16 is fastest.  sum may be x or residual, y may be x or
  * residual, not both the same; other overlaps of what is written are refused.  A row whose squares pass float32's range gives zeros, one
- * with an infinity or NaN gives NaN where it stands.
+ * with an infinity zeros and NaN where it stands, one with a NaN gives NaN throughout.
  *
  * sbnet_rms_norm_i8_on_tiles: the same s, and y in 8 bits, as sbnet_quantize_i8_on_tiles makes them of the unrounded
  * (fp32) y.  codes: int8 [cap][pixels][pitch], scales: float32 [cap][pixels].
@@ -502,6 +502,8 @@ sbnet_status sbnet_quantize_i8_on_tiles(const void *x, sbnet_dtype dtype, const 
  * the tiles b < min(*count, cap):
  *   dx = r * (gain * dy - h * mean over c of (gain * dy * h)) + dsum    (the gradient of x and of the residual),
  *   dgain[c] = sum over the rows of dy * h                              (device float32 [C], written; zeros without rows).
+ * A row whose squares pass float32's range, of which the norm is zeros, gives dx = dsum (or zeros) and adds nothing to dgain; one with an infinity or
+ * NaN gives NaN throughout.
  * fp32 sums and arithmetic, dx rounded once to `dtype`; C at most 32768; dgain's sums in a fixed order, no atomics: the same bits every
  * run for a given cap.  s, dy, dsum, dx: [cap][pixels][C]; later tiles of dx are not touched; dx may be s, dy or dsum (the
  * whole stack; other overlaps are refused).  workspace: device, 4-byte aligned, sbnet_rms_norm_backward_workspace_bytes(cap, pixels, C)

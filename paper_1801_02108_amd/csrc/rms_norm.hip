@@ -132,7 +132,7 @@ template <class V, int T, int P>
 __global__ __launch_bounds__(wg_threads(T)) void rms_backward_rows(BackArgs p) {
     constexpr int E = V::E, NV = P / E, RB = wg_threads(T) / T;
     constexpr bool kKeep = P <= 16;
-    __shared__ uint32_t slots[2][2][16];
+    __shared__ uint32_t slots[2][3][16];
     __shared__ float sums[RB > 1 ? RB * T * P : 1];
     const long long rows = active_rows(p.count, p.cap, p.pixels);
     const int t = threadIdx.x % T;
@@ -178,7 +178,14 @@ __global__ __launch_bounds__(wg_threads(T)) void rms_backward_rows(BackArgs p) {
             }
         }
         over_row2<T>(ss, gs, slots[turn][0], slots[turn][1]);
-        const float r = rsqrtf(ss * p.inv_c + p.eps), m = gs * p.inv_c * r;
+        const float r = rsqrtf(ss * p.inv_c + p.eps);
+        float m = gs * p.inv_c * r;
+        if (r == 0.f) {                                           // the squares pass the range: y = 0 there and so is dx, unless the row holds an infinity
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < P; ++k) top = max(top, __float_as_uint(s[k / E].get(k % E)) & 0x7fffffffu);
+            m = over_row<T>(top, MaxU32(), slots[turn][2]) < kInfBits ? 0.f : __uint_as_float(0x7fc00000u);
+        }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * T + t) * E;

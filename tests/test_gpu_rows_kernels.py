@@ -192,3 +192,45 @@ def test_norms_on_a_few_tiles_of_a_long_list(cap, pixels, C, dtype):
         terms = few[2].double() * h
         chain = n * pixels / 128 + 32 + 512 / 16 + 16 + 32
         assert ((dgain.double() - terms.sum((0, 1))).abs() <= terms.abs().sum((0, 1)) * chain * U).all()
+
+
+@pytest.mark.parametrize("C", [64, 97, 2048])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_of_rows_whose_squares_pass_the_range_of_float32(dtype, C):
+    """The norm gives zeros for such a row, whatever it holds: its gradients are zeros too (and the one past the norm), also where the sum of
+    gain dy s passes the range."""
+    step("rows past the range %d %s" % (C, dtype))
+    g = torch.Generator(device="cuda").manual_seed(C)
+    s, dy, ds = (torch.randn((6, 1, C), generator=g, device="cuda").to(TORCH_DT[dtype]) for _ in range(3))
+    s[1], dy[1] = 2e38, 2.0                       # the sum is infinite
+    s[3], dy[3] = 2e38, 2.0                       # ... of both signs, no number
+    s[3, 0, C // 2:] = -2e38
+    s[4, 0, 0] = 1e30                             # only the squares are
+    assert not sb.rms_norm_on_tiles(s, cnt(6))[0][[1, 3, 4]].any()
+    few = [0, 2, 5]
+    for extra in (None, ds):
+        dx, dgain = sb.rms_norm_backward_on_tiles(s, dy, cnt(6), dsum=extra)
+        for k in (1, 3, 4):
+            assert torch.equal(dx[k], torch.zeros_like(dx[k]) if extra is None else extra[k])
+        dx1, dgain1 = sb.rms_norm_backward_on_tiles(s[few], dy[few], cnt(3), dsum=None if extra is None else extra[few])
+        assert torch.equal(dx[few], dx1)
+        terms = dy[few].double() * s[few].double() / (s[few].double().square().mean(-1, keepdim=True) + 1e-6).sqrt()
+        assert ((dgain - dgain1).double().abs() <= terms.abs().sum((0, 1)) * 2 * (6 + 32) * U).all()      # (another order of the same sums)
+
+
+@pytest.mark.parametrize("C", [64, 97, 2048, 20000])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_gradients_of_rows_with_an_infinity_or_nan(dtype, C):
+    """As the formula has it: no number in the whole row, and in dgain where the value stands (a NaN: everywhere); no other row."""
+    step("infinities in gradients %d %s" % (C, dtype))
+    g = torch.Generator(device="cuda").manual_seed(C)
+    s, dy = (torch.randn((5, 1, C), generator=g, device="cuda").to(TORCH_DT[dtype]) for _ in range(2))
+    clean = sb.rms_norm_backward_on_tiles(s, dy, cnt(5))[0]
+    for at, v in ((0, float("inf")), (C - 1, float("-inf")), (C // 2, float("nan"))):
+        bad = s.clone()
+        bad[2, 0, at] = v
+        dx, dgain = sb.rms_norm_backward_on_tiles(bad, dy, cnt(5))
+        assert dx[2].isnan().all() and torch.equal(dx[[0, 1, 3, 4]], clean[[0, 1, 3, 4]])
+        want = torch.full((C,), v != v, device="cuda")
+        want[at] = True
+        assert torch.equal(dgain.isnan(), want)
