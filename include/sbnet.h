@@ -475,7 +475,7 @@ sbnet_status sbnet_conv_on_tiles_f8(const void *tiles_in_f8, const int32_t *coun
  * x, residual, sum, y: [cap][pixels][C] in `dtype` (F32, BF16 or F16); residual and sum are both given or both NULL;
  * gain: device float32 [C] or NULL (1); eps a normal float32 number above 0.  C at most 32768; pointers need their element's
  * alignment only, 16 bytes with C * element size a multiple of 16 is fastest.  sum may be x or residual, y may be x or
- * residual, not both the same; other overlaps of what is written are refused.  A row whose squares pass float32's range gives zeros, one
+ * residual, not both the same; other overlaps of what is written, with count too, are refused.  A row whose squares pass float32's range gives zeros, one
  * with an infinity zeros and NaN where it stands, one with a NaN gives NaN throughout.
  *
  * sbnet_rms_norm_i8_on_tiles: the same s, and y in 8 bits, as sbnet_quantize_i8_on_tiles makes them of the unrounded

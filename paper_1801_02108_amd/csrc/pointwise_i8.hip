@@ -660,7 +660,7 @@ extern "C" sbnet_status sbnet_pointwise_i8_on_tiles(const int8_t *codes, const f
     const size_t rows = (size_t)cap * pixels, ob = rows * Cout * elem_bytes(dtype);
     if (ranges_overlap(out, ob, codes, rows * pitch) || ranges_overlap(out, ob, scales, rows * 4) ||
         ranges_overlap(out, ob, w_codes, (size_t)Cout * pitch) || ranges_overlap(out, ob, w_scales, (size_t)Cout * 4) ||
-        (bias && ranges_overlap(out, ob, bias, (size_t)Cout * 4)))
+        (bias && ranges_overlap(out, ob, bias, (size_t)Cout * 4)) || holds_count(out, ob, count))
         return fail(SBNET_EINVAL, "%s: out overlaps an input", who);
     if (cap == 0) return SBNET_OK;
     PointArgs p = {};

@@ -374,6 +374,9 @@ sbnet_status rows_launch(const char *who, Form form, const void *x, const void *
                 return fail(SBNET_EINVAL, "%s: stacks overlap", who);
         if (ranges_overlap(codes, rows * pitch, scales, rows * 4)) return fail(SBNET_EINVAL, "%s: stacks overlap", who);
     }
+    if (holds_count(sum, bytes, count) || holds_count(y, bytes, count) || holds_count(codes, rows * pitch, count) ||
+        holds_count(scales, rows * 4, count))
+        return fail(SBNET_EINVAL, "%s: a result overlaps count", who);
     if (cap == 0) return SBNET_OK;
     RowArgs p = {};
     p.x = x; p.res = residual; p.sum = sum; p.y = y; p.codes = codes; p.scales = scales; p.gain = gain; p.count = count;
@@ -442,6 +445,8 @@ extern "C" sbnet_status sbnet_rms_norm_backward_on_tiles(const void *s, const vo
     if (gain && (ranges_overlap(dx, bytes, gain, cb) || ranges_overlap(dgain, cb, gain, cb) || ranges_overlap(workspace, need, gain, cb)))
         return fail(SBNET_EINVAL, "%s: a result or the workspace overlaps gain", who);
     if (ranges_overlap(dgain, cb, workspace, need)) return fail(SBNET_EINVAL, "%s: workspace overlaps dgain", who);
+    if (holds_count(dx, bytes, count) || holds_count(dgain, cb, count) || holds_count(workspace, need, count))
+        return fail(SBNET_EINVAL, "%s: a result or the workspace overlaps count", who);
     BackArgs p = {};
     p.s = s; p.dy = dy; p.dsum = dsum; p.dx = dx; p.gain = gain; p.count = count;
     p.eps = eps; p.inv_c = 1.f / (float)C; p.cap = cap; p.pixels = pixels; p.C = C;

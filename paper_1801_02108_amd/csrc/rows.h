@@ -10,6 +10,9 @@ __device__ __forceinline__ long long active_rows(const int32_t *count, int cap, 
     return n > 0 ? (long long)n * pixels : 0;
 }
 
+// whether what a call writes holds its count, which the kernels read while others write
+inline bool holds_count(const void *q, size_t bytes, const int32_t *count) { return q && ranges_overlap(q, bytes, count, sizeof(int32_t)); }
+
 constexpr float kLeastTop = 7.888609052210118e-31f;                  // 2^-100
 constexpr uint32_t kInfBits = 0x7f800000u;
 
