@@ -540,6 +540,7 @@ sbnet_status direct_go(const char *who, const PointArgs &p, long long rows, hipS
     return launch_status(who);
 }
 
+constexpr int kLds = 160 * 1024;
 size_t stream_lds(int KC, int N) {
     const size_t groups = (N + 63) / 64;
     return groups * (KC * 4096 + 512);
@@ -548,7 +549,8 @@ template <int DT, int KC>
 sbnet_status stream_go(const char *who, const PointArgs &p, long long rows, hipStream_t s) {
     const long long steps = (rows + 15) / 16;
     const size_t lds = stream_lds(KC, p.N);
-    (void)hipFuncSetAttribute((const void *)i8_stream<DT, KC>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    // (the same for every layer: another thread's call may come between this one and the launch)
+    (void)hipFuncSetAttribute((const void *)i8_stream<DT, KC>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     hipLaunchKernelGGL((i8_stream<DT, KC>), dim3((unsigned)(steps < 256 ? steps : 256)), dim3(64 * kStreamWaves), lds, s, p, (p.N + 63) / 64);
     return launch_status(who);
 }
@@ -585,7 +587,7 @@ int cheapest(long long rows, int N, int pitch) {
 // 5.4 and 5.2, 20000 6.7 and 9.4; 256 -> 256, 16000 8.5 and 7.3, 30000 10.2 and 13.1; 64 -> 1024, 8192 12.9 and 9.7, 30000 15.3 and 24.9.  From 385 input
 // channels on the rows in flight are fewer: 512 -> 64, 20000 6.8 and 7.2, 512 -> 128, 50000 13.8 and 13.0.)
 bool streams(long long rows, int N, int KC) {
-    if (KC > 8 || stream_lds(KC <= 4 ? KC : KC <= 6 ? 6 : 8, N) > 160 * 1024) return false;
+    if (KC > 8 || stream_lds(KC <= 4 ? KC : KC <= 6 ? 6 : 8, N) > kLds) return false;
     const long long weights = (long long)KC * N;
     return rows >= (KC <= 6 ? 4000 + 14 * weights : 60 * weights);
 }

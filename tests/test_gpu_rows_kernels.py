@@ -6,6 +6,7 @@ the row's scale and the fused step with channel scale and bias round to 24 bits 
 of the product without the bias, half a step of the result's type (bf16 2^-8, f16 2^-11, f32 2^-24) of the value with it, and 2^-25
 for f16 values below its normal range; 1.01 is for the bounds being taken of rounded values."""
 import re
+import threading
 
 import numpy as np
 import pytest
@@ -234,3 +235,35 @@ def test_gradients_of_rows_with_an_infinity_or_nan(dtype, C):
         want = torch.full((C,), v != v, device="cuda")
         want[at] = True
         assert torch.equal(dgain.isnan(), want)
+
+
+def test_two_threads_with_layers_of_different_widths():
+    """Layers of one kernel that need different amounts of LDS, from two threads on streams of their own."""
+    step("two threads")
+    jobs = []
+    for N in (64, 512):
+        codes, scales, w, ws, bias = product_inputs(130, 256, 256, N)
+        n = cnt(130)
+        assert product_kernel(lambda: sb.pointwise_i8_on_tiles(codes, scales, n, w, ws, bias=bias)) == ("i8_stream", 4)
+        want = sb.pointwise_i8_on_tiles(codes, scales, n, w, ws, bias=bias)
+        jobs.append((codes, scales, n, w, ws, bias, want, torch.empty_like(want)))
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(job, stream):
+        codes, scales, n, w, ws, bias, want, out = job
+        try:
+            with torch.cuda.stream(stream):
+                for _ in range(500):
+                    sb.pointwise_i8_on_tiles(codes, scales, n, w, ws, bias=bias, out=out)
+            stream.synchronize()
+            assert torch.equal(out, want)
+        except Exception as e:                    # handed to the main thread
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(job, torch.cuda.Stream())) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors

@@ -1,5 +1,8 @@
-"""More of what the calls on rows refuse on the host (nothing is launched: the device addresses are made up)."""
+"""More of what the calls on rows do on the host: what they refuse and what they ask of the runtime (nothing is launched: the device addresses are made up)."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -52,3 +55,35 @@ def test_a_count_inside_what_a_call_writes_is_refused(k):
     assert call(count) == sb.EINVAL
     text = sb.lib().sbnet_last_error().decode()
     assert "count" in text or "out overlaps an input" in text, text
+
+
+RECORDER = """
+#include <stdio.h>
+int hipFuncSetAttribute(const void *f, int attribute, int value) { printf("%p %d %d\\n", f, attribute, value); fflush(stdout); return 0; }
+int hipLaunchKernel(void) { return 0; }
+int hipGetLastError(void) { return 0; }
+"""
+CHILD = """
+import ctypes, sys
+ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)
+lib = ctypes.CDLL(sys.argv[2])
+P, I = ctypes.c_void_p, ctypes.c_int
+call = lib.sbnet_pointwise_i8_on_tiles
+call.argtypes = [P, P, P, I, I, I, P, P, P, I, I, I, P, P]
+a = [0x7f0000000000 + (k << 32) for k in range(6)]
+for cout in (64, 512, 128, 40):
+    assert call(a[0], a[1], a[2], 200, 256, 256, a[3], a[4], None, cout, 0, 1, a[5], None) == 0
+"""
+
+
+def test_layers_of_one_kernel_ask_for_the_same_lds(tmp_path):
+    """The amount is an attribute of the kernel, so that of a layer must not be what another thread's layer sets between.  The runtime's calls are
+    taken by a recorder: no device is touched."""
+    (tmp_path / "recorder.c").write_text(RECORDER)
+    subprocess.check_call(["gcc", "-shared", "-fPIC", "-o", str(tmp_path / "recorder.so"), str(tmp_path / "recorder.c")])
+    env = dict(os.environ, HIP_VISIBLE_DEVICES="", ROCR_VISIBLE_DEVICES="")
+    r = subprocess.run([sys.executable, "-c", CHILD, str(tmp_path / "recorder.so"), sb.LIB_PATH], env=env, capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0, r.stderr
+    calls = [line.split() for line in r.stdout.splitlines()]
+    assert len(calls) == 4 and len(set(map(tuple, calls))) == 1, r.stdout
+    assert int(calls[0][2]) == 160 * 1024
