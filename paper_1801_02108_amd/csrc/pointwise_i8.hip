@@ -305,7 +305,8 @@ void i8_tiles(PointArgs p) {
 // ---- small products: 16 MT rows x 16 NT channels per workgroup, operands from memory to registers, the channels summed over split between its waves
 // 16 x 16 x 64 steps, weights as the first operand again.  Wave w of KS takes the pieces of 128 bytes w, w + KS, ... of every row; the waves' sums
 // meet in LDS.  Frag n of NT holds channels 4 NT q + 4 n + r in its row 4 q + r, which gives a lane 4 NT neighbouring channels.
-// Bound by latency (few rows: by the weights' bytes): every wave has U pieces of all its rows in flight, twice.  1 x 4096 x 4096: 5.4 us, 2.7 of them
+// Bound by latency (few rows: by the weights' bytes): a wave requests U pieces of all its rows and, before it multiplies them, the next U.  (That request is behind
+// a branch, so that the waits count it as not made: all of it has landed before the last step of the first U.)  1 x 4096 x 4096: 5.4 us, 2.7 of them
 // the launch, 6 TB/s for the rest; 23 x 2056 x 5125 5.8 us; 300 x 368 x 360 4.1 us.
 __device__ __forceinline__ i32x4 mfma_i8_16(uint4 a, uint4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
@@ -414,12 +415,14 @@ __global__ __launch_bounds__(64 * KS) void i8_direct(PointArgs p) {
 // 16 x 16 x 64 steps on 64 channels at a time.  The weights are laid out in LDS as the operand reads take them, 1 KB each, once a workgroup.  Frags 2 s
 // and 2 s + 1 hold channels 32 s + 8 q + 4 (n % 2) + r in their rows 4 q + r: a lane's pair is 8 neighbouring channels, and one 16-byte store of
 // a wave is 64 bytes of each of 16 rows.
-// Bound by memory: the next 16 rows are requested before these are multiplied, by twelve waves a CU (eight waves of 32 rows: 112640 x 256 x 256
-// 22.0 us instead of 20.2, 142560 x 256 x 64 13.3 and 12.6, which is 4.4 TB/s).
+// Bound by memory, which twelve waves a CU keep busy (eight waves of 32 rows: 112640 x 256 x 256 22.0 us instead of 20.2, 142560 x 256 x 64 13.3 and 12.6, which is
+// 4.4 TB/s).  A wave requests the next 16 rows before it multiplies these, but it also waits for them there: the loop over the groups stores, and in front of
+// it nothing may be outstanding.  So the overlap is between waves, not within one.
 //
 // Results no wider than the input (in channels) are written past the cache, which is left to the codes, in whole lines: 112640 x 128 x 128 11.9 us and, with a
 // pass over the results behind it, 21.5; so 8.9 and 21.0; 142560 x 256 x 64 13.1 and 20.0, 12.0 and 20.0; 112640 x 256 x 256 21.4 and 40.0, 18.7 and 39.3.
-// Wider ones gain alone and lose with who reads them: 60000 x 64 x 512 15.8 and 34.0, 14.4 and 35.5.
+// Wider ones gain alone and lose with who reads them: 60000 x 64 x 512 15.8 and 34.0, 14.4 and 35.5.  Short lists neither gain nor lose: 20000 x 256 x 64 4.5
+// and 8.4, past the cache 4.4 and 8.3; 12000 x 128 x 128 4.4 and 8.2, 4.6 and 8.3; 40000 x 128 x 128 6.1 and 10.3, 5.2 and 9.8.
 constexpr int kStreamWaves = 12;
 
 // lanes 8 .. 15 of each 16 of a with lanes 0 .. 7 of b
@@ -567,6 +570,8 @@ struct Shape {
 constexpr Shape kShapes[] = {{16, 16, 0.95f, 500}, {16, 32, 1.4f, 600}, {32, 16, 1.4f, 600}, {32, 32, 1.85f, 450},
                              {64, 64, 2.0f, 800}, {64, 128, 2.35f, 1000}, {128, 128, 3.15f, 2000}, {256, 128, 5.4f, 4000}};
 
+// `rows` are those of the list's capacity, here and for the streamed lists: a list with few active tiles takes the tile of a full one (64 pixels of 1024 -> 256,
+// 55 of 550 tiles active: 8.6 us, a list of 55 5.3; 1024 -> 2048, 14 of 140: 8.7 and 6.6; 324 pixels of 256 -> 64, 219 of 2200: 6.5 and 6.6).
 int cheapest(long long rows, int N, int pitch) {
     int best = 0;
     float least = 0.f;

@@ -1,13 +1,17 @@
 // Root-mean-square norm over a pixel's channels with the residual's addition, its 8-bit form, its gradients, and the row
 // quantiser that the 8-bit form shares (sbnet_rms_norm_on_tiles and its neighbours in sbnet.h).
 //
-//   rms_rows           s = x + residual, r = rsqrt(mean(s^2) + eps), y = s r gain; in 8 bits: y / scale, scale = max|y| / 127
+//   rms_rows           s = x + residual, r = rsqrt(mean(s^2) + eps), y = s r gain; in 8 bits: round(y (127 (1 / t))), scale t / 127,
+//                      t = max|y| or 2^-100
 //   rms_backward_rows  with h = s r:  dx = r (gain dy - h mean(gain dy h)) + dsum,  partial sums of dgain = dy h
 //   rms_dgain_sum      adds the partial sums in a fixed order
 //
 // Bound by memory: a row is read once, stays in registers over its sums, and is written once.  112640 rows of 256 bf16: with the residual 40 us (5.8 TB/s; a
 // large copy reaches 5.0), in 8 bits from 44288 rows of 384 21 to 24 us (5.0 to 5.7 TB/s), without a norm from 142560 of 256 18 to 21 us (5.3 to 6.2 TB/s);
 // gradients with the one past the norm 41 us (5.6 TB/s) and 4 for the sums of dgain; 4099 rows of 4096 f32 22 us (6.1 TB/s).
+// Of rows of more than 16384 channels a thread holds 32 in 128 registers.  The norm fits (single f32 and bf16 elements: all but 1 to 10 of them; 800 x 32768 bf16
+// with the residual 41 us, 5.1 TB/s), the gradients do not: 52 to 312 bytes a lane go through scratch memory (the same rows 77 us, 2.0 TB/s; 1000 x 20001 f16
+// by single elements 175, 0.7 TB/s).
 #include "rows.h"
 
 namespace sbnet {
@@ -127,7 +131,7 @@ struct BackArgs {
 };
 
 // A thread keeps its channels' sums of dy h over all its rows; the workgroup adds those of its rows' places in ascending order.  With 32 channels a
-// thread the gains, and the gradient past the norm until it is added, stay in memory: the registers hold no more.
+// thread the gains, and the gradient past the norm until it is added, stay in memory: 512 threads of them then fit their registers, 1024 still do not.
 template <class V, int T, int P>
 __global__ __launch_bounds__(wg_threads(T)) void rms_backward_rows(BackArgs p) {
     constexpr int E = V::E, NV = P / E, RB = wg_threads(T) / T;
@@ -262,7 +266,9 @@ __global__ __launch_bounds__(1024) void rms_dgain_sum(const float *__restrict__ 
 
 // Threads and channels per thread by the row's width, f(T, P) as types: lanes of a wave while 16 channels a lane hold the row, a workgroup's threads
 // beyond.  (Row quantiser, 3000 rows of 8192: 512 threads of 16 channels 13.8 us, 1024 of 8 16.2; 256 of 32 13.4, but one row then takes 3.4 instead of
-// 3.1.  Norm of 14000 rows of 2048: 128 of 16 42.6, 256 of 8 42.2, 64 of 32 41.4, and 23 rows of 2056 in 8 bits 3.8, 3.8 and 4.2.)
+// 3.1.  Norm of 14000 rows of 2048: 128 of 16 42.6, 256 of 8 42.2, 64 of 32 41.4, and 23 rows of 2056 in 8 bits 3.8, 3.8 and 4.2.)  From 8193 channels on 512 threads of 32 and 1024 of 16: norm with
+// residual of 1500 rows of 16384 bf16 34.6 and 35.4, of 10000 19.8 and 20.2, quantiser 12.6 and 13.2, 9.0 and 10.0; the gradients, for which the split is the
+// same, would take 35.7 instead of 42.9, and 45.1 instead of 69.7 by single elements (1700 x 14001 f16).  From 16385 on no other split holds a row.
 template <int A, int B> struct Split {
     static constexpr int T = A, P = B;
 };
@@ -341,9 +347,12 @@ void back_go(bool wide, const BackArgs &p, int grid, hipStream_t s) {
 }
 
 // Whether a call's stacks pass four fifths of the 256 MiB last-level cache: then its results are written past it, for they would be gone before they are read
-// again.  (Norm with residual of 112640 x 256 bf16, 231 MB: 44.4 us and, with the sum of both results behind it, 71.1; past the cache 41.5 and 68.8.  Below the
-// line the norm alone gains too, and who reads its results loses more: 44288 x 384 in 8 bits, 119 MB, 26.7 and 22.1 us, with the layer and the norm behind it
-// 70.7 and 73.8; 112640 x 256 in 8 bits, 202 MB, 40.4 and 38.9, 101 and 103.)
+// again.  (us, through the cache and past it, results to other memory each time, in brackets with a sum of both results behind it.  Norm with residual: 112640 x 256
+// bf16, 231 MB, 42.8 and 41.0 (68.7, 69.1); 160000 x 256 60.4 and 58.6 (98.6, 102.2); 250000 x 256 94.1 and 91.3 (155.5, 160.4).  In 8 bits, with the product
+// behind it: 160000 x 256 60.7 and 59.7, 250000 x 256 94.9 and 90.7.  Results that go to the same memory every time stay in the cache up to about 300 MB: 130000
+// x 256 41.5 and 46.7.  Below the line who reads the results loses more: 44288 x 384 in 8 bits, 119 MB, 26.7 and 22.1 us, with the layer and the norm behind it
+// 70.7 and 73.8; 112640 x 256 in 8 bits, 202 MB, 40.4 and 38.9, 101 and 103.)  The stacks count with their capacity: 219 active of 2200 tiles of 324 x 256 take
+// 22.5 and, with a norm of the results behind it, 47.6; a list of 219, which goes through the cache, 22.8 and 46.7.
 bool large_call(size_t bytes) { return bytes >= ((size_t)1 << 28) / 5 * 4; }
 
 sbnet_status rows_launch(const char *who, Form form, const void *x, const void *residual, sbnet_dtype dtype, const int32_t *count,
